@@ -16,8 +16,9 @@
  *    failed validation returns a negative status and enqueues nothing.
  *  - Data errors found on the device (a NaN score, a non-finite K/V value) are
  *    OR-ed into the caller's device status word (bit 0: NaN score, bit 1:
- *    non-finite K/V, bit 2: slot index outside [0, T)); read it after the
- *    stream is synchronized.
+ *    non-finite K/V, bit 2: slot index outside [0, T), or an index of the
+ *    paged cache out of range, bit 3: not enough free pages); read it after
+ *    the stream is synchronized.
  *  - A semkv_cache is a plain host struct: configuration, device pointers and
  *    host-side counts.  Calls on one cache must be serialized on one stream.
  *    Calls on different caches are independent.
@@ -46,7 +47,7 @@ enum {
 };
 
 enum { SEMKV_BASE_AFFINE = 0, SEMKV_BASE_TQ = 1, SEMKV_BASE_ROT_AFFINE = 2 };
-enum { SEMKV_STATUS_NAN_SCORE = 1, SEMKV_STATUS_NONFINITE_KV = 2, SEMKV_STATUS_BAD_INDEX = 4 };
+enum { SEMKV_STATUS_NAN_SCORE = 1, SEMKV_STATUS_NONFINITE_KV = 2, SEMKV_STATUS_BAD_INDEX = 4, SEMKV_STATUS_NO_PAGES = 8 };
 
 /* Configuration of one cache.
  *  base:   SEMKV_BASE_AFFINE -- per group of `group` channels, an asymmetric
@@ -287,7 +288,7 @@ int semkv_dequant(const semkv_cache* c, int32_t layer, float* k_hat, float* v_ha
  * Sums run in fp32 (the score's relative error is below 1e-5 for d <= 8192).
  * A non-finite state gives a non-finite score, which semkv_rank reports. */
 enum { SEMKV_IND_DELTA_NORM = 0, SEMKV_IND_NORM = 1, SEMKV_IND_VARIANCE = 2, SEMKV_IND_COSINE_DELTA = 3 };
-enum { SEMKV_DTYPE_F16 = 0, SEMKV_DTYPE_BF16 = 1 };
+enum { SEMKV_DTYPE_F16 = 0, SEMKV_DTYPE_BF16 = 1, SEMKV_DTYPE_F32 = 2 };
 int semkv_score_hidden(int32_t indicator, const void* hidden, int32_t dtype, int32_t m, int32_t batch,
                        int64_t T, int32_t d_model, int64_t s_state, int64_t s_batch, int64_t s_token,
                        float* scores, hipStream_t stream);
@@ -299,6 +300,168 @@ int semkv_score_hidden(int32_t indicator, const void* hidden, int32_t dtype, int
  * fp32 [batch][T]. */
 int semkv_score_kv_norm(const semkv_cache* c, const uint16_t* X, int64_t sL, int64_t sB, int64_t sH,
                         int64_t sT, int64_t T, float* scores, hipStream_t stream);
+
+/* ---- Paged cache held in 4 bits ----------------------------------------
+ * Sequences of different and growing lengths at one uniform precision: every
+ * K and V row is kept at 16 levels by the affine quantizer above (L = 16, per
+ * group of `group` channels: zero = fp16(min), scale = fp16((max - zero)/15),
+ * both saturated to +-65504, codes clamp(rint((x - zero) * (1/scale)), 0, 15)
+ * in fp32 with the stored pair, 0 where scale is 0; value fmaf(c, scale,
+ * zero)), in pages of 64 tokens that sequences take from a common pool.
+ *
+ * Lengths, page tables and the pages' reference counts live on the device:
+ * every call below enqueues kernels only and reads nothing back, so a decode
+ * loop that takes pages as it grows can be captured into a graph.  Data
+ * errors go to the status word; nothing is read or written out of range.
+ *
+ *  n_q_heads: a multiple of n_kv_heads, at most 64 query heads to a kv head.
+ *  head_dim:  64 or 128.  group: 32, 64 or 128, at most head_dim.
+ *  n_pages:   pages of the pool, at most 2^20.
+ *  max_seqs:  sequence slots, at most 1024.
+ *  seq_pages: pages one sequence may hold, at most 2^20 (max_seqs * seq_pages
+ *             at most 2^28; n_layers * n_kv_heads at most 65535). */
+typedef struct semkv_paged_config {
+  int32_t n_layers, n_kv_heads, n_q_heads, head_dim, group;
+  int32_t n_pages, max_seqs, seq_pages;
+} semkv_paged_config;
+
+/* Layout.
+ *  pool:  [n_pages][n_layers][n_kv_heads] records of record_bytes: 64 tokens'
+ *         K codes (32 head_dim bytes), V codes (same), K metadata, V metadata
+ *         (head_dim/group * 256 bytes each: fp16 {scale, zero} at
+ *         [group][token]).  Codes are 4 bits, 8 to a 32-bit word, slot j at
+ *         bits 4 (j div 2 + 4 (j mod 2)), in pieces of 64 lanes x 4 words:
+ *           K word (piece p, lane, w), x = 4p + w, D' = head_dim/32: token
+ *             16 (x div D') + lane mod 16, channel 32 (x mod D') +
+ *             8 (lane div 16) + j
+ *           V word (piece p, lane, w), x = 4p + w: channel 16 (x div 2) +
+ *             lane mod 16, token 32 (x mod 2) + 16 (j div 4) +
+ *             4 (lane div 16) + j mod 4
+ *  state: int32 words.  Word 0: not 0 after a semkv_paged_reserve that did not
+ *         find its pages.  lens_word: [max_seqs] tokens of each sequence;
+ *         table_word: [max_seqs][seq_pages] page of tokens 64c .. 64c+63, -1
+ *         where none; refs_word: [n_pages] table entries that name the page;
+ *         free_word: bit p%32 of word p/32 set iff page p is free; then
+ *         scratch.  Readable by the caller; written by the calls only.
+ *  workspace: scratch of semkv_paged_attn; needs no clearing. */
+typedef struct semkv_paged_sizes {
+  size_t pool_bytes, state_bytes, workspace_bytes;
+  int64_t record_bytes, page_bytes, lens_word, table_word, refs_word, free_word, scratch_word;
+} semkv_paged_sizes;
+
+typedef struct semkv_paged {
+  semkv_paged_config cfg;
+  semkv_paged_sizes sz;
+  uint8_t* pool;    /* device, 16-byte aligned */
+  int32_t* state;   /* device, 16-byte aligned */
+  int32_t* status;  /* device status word */
+} semkv_paged;
+
+int semkv_paged_cache_sizes(const semkv_paged_config* cfg, semkv_paged_sizes* out);
+
+/* Initialize `c` over caller buffers and enqueue the emptying of `state`: no
+ * sequence holds a token, every page is free.  The pool needs no clearing. */
+int semkv_paged_init(semkv_paged* c, const semkv_paged_config* cfg, void* pool, int32_t* state, int32_t* status,
+                     hipStream_t stream);
+
+/* Take over lengths and page tables (a saved cache, or tables managed by the
+ * caller): lens device int32 [max_seqs], table device int32
+ * [max_seqs][seq_pages], entry c of a row used where 64c < its length.
+ * Counts and free pages follow.  A length outside [0, 64 seq_pages] is
+ * clamped, an entry outside [0, n_pages) becomes -1 (SEMKV_STATUS_BAD_INDEX):
+ * its tokens are not cached. */
+int semkv_paged_assign(semkv_paged* c, const int32_t* lens, const int32_t* table, hipStream_t stream);
+
+/* Room for n_new[s] more tokens of every sequence s (device int32
+ * [max_seqs], 0 or more): its length grows by n_new[s] and it gets the
+ * lowest-numbered free pages, sequences in ascending order.  Where the new
+ * tokens start inside a page that other sequences hold too, the sequence first
+ * gets a copy of it (if every holder grows, the lowest keeps the original).
+ * If the free pages or seq_pages do not suffice, nothing changes,
+ * SEMKV_STATUS_NO_PAGES is set, and semkv_paged_write stores nothing until a
+ * semkv_paged_reserve succeeds.  A negative count is taken as 0
+ * (SEMKV_STATUS_BAD_INDEX). */
+int semkv_paged_reserve(semkv_paged* c, const int32_t* n_new, hipStream_t stream);
+
+/* Every slot s takes over the contents that slot parent[s] had before the call
+ * (device int32 [max_seqs]): pages are shared, not copied.  parent[s] = s
+ * keeps s as it is, -1 empties it.  Pages that no slot holds any more are
+ * free.  An entry outside [-1, max_seqs) is taken as s
+ * (SEMKV_STATUS_BAD_INDEX). */
+int semkv_paged_fork(semkv_paged* c, const int32_t* parent, hipStream_t stream);
+
+/* Sequence s keeps the tokens keep[s][0 .. n_keep[s]) only, in that order
+ * (device int32, rows of ld_keep entries; semkv_rank's slot lists are such
+ * lists): their codes move as they are into fresh pages (the lowest-numbered
+ * free ones, sequences in ascending order), its length becomes n_keep[s] and
+ * its former pages are released.  n_keep[s] = -1 leaves s as it is.  If the
+ * free pages do not suffice, nothing changes and SEMKV_STATUS_NO_PAGES is
+ * set.  n_keep[s] outside [-1, min(ld_keep, 64 seq_pages)] is taken as -1, a
+ * position outside the sequence gives a row of zeros
+ * (SEMKV_STATUS_BAD_INDEX). */
+int semkv_paged_compact(semkv_paged* c, const int32_t* keep, int64_t ld_keep, const int32_t* n_keep,
+                        hipStream_t stream);
+
+/* The rows of a call are the last tokens of sequences 0 .. n_seqs-1: those of
+ * sequence s are rows starts[s] .. starts[s+1]-1 (device int32 [n_seqs+1],
+ * ascending), its last starts[s+1]-starts[s] tokens in order; n_rows bounds
+ * them all (at most 2^28).  Rows from starts[n_seqs] on (a padded batch) are neither read nor
+ * written.  Starts that descend or pass n_rows set SEMKV_STATUS_BAD_INDEX, and
+ * the sequence has no row.
+ *
+ * Quantize rows of K and V into the pages: element (row t, kv head h, channel
+ * j) at t*sT + h*sH + j (+ l*sL with layer == -1, every layer), dtype
+ * SEMKV_DTYPE_F16 or _BF16, 16-byte aligned, strides multiples of 8.  A group
+ * with a value that is not finite is stored as zeros and sets
+ * SEMKV_STATUS_NONFINITE_KV.  Rows whose page is missing or held by another
+ * sequence too are not stored (SEMKV_STATUS_BAD_INDEX). */
+int semkv_paged_write(semkv_paged* c, int32_t layer, const void* K, const void* V, int32_t dtype, int64_t sL, int64_t sT,
+                      int64_t sH, const int32_t* starts, int32_t n_seqs, int64_t n_rows, hipStream_t stream);
+
+/* The values that the pages hold for these rows: K and V contiguous
+ * [n_rows][n_kv_heads][head_dim] (layer == -1: [n_layers] of them), dtype F16,
+ * BF16 or F32, 16-byte aligned.  A row whose page is missing, or that would
+ * precede its sequence's first token, is zeros. */
+int semkv_paged_read(const semkv_paged* c, int32_t layer, void* K, void* V, int32_t dtype, const int32_t* starts,
+                     int32_t n_seqs, int64_t n_rows, hipStream_t stream);
+
+/* Causal attention of these rows over their sequences' pages: row i of the m
+ * rows of a sequence of n tokens attends to its tokens 0 .. n-m+i,
+ *   out = softmax(scale q . k_t) . v_t,  lse = ln sum_t exp(scale q . k_t)
+ * over the values that semkv_paged_read gives.  A row that sees no token (an
+ * empty sequence, missing pages) gives out 0 and lse -inf.
+ * q: element (row t, query head h, channel j) at t*sT + h*sH + j, dtype F16 or
+ * BF16, 16-byte aligned, strides multiples of 8, |q| below 2^100; out: the
+ * same dtype, contiguous [n_rows][n_q_heads][head_dim], 16-byte aligned; lse:
+ * fp32 [n_rows][n_q_heads] or NULL.  scale: positive and finite.
+ * workspace: ws_bytes >= sizes.workspace_bytes, 16-byte aligned; calls that
+ * overlap in time need one each. */
+int semkv_paged_attn(const semkv_paged* c, int32_t layer, const void* q, int32_t dtype, int64_t sT, int64_t sH,
+                     float scale, const int32_t* starts, int32_t n_seqs, int64_t n_rows, void* out, float* lse,
+                     void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Log probabilities of given tokens (Sec. 3.3's self-information is their
+ * negative), for [batch][T] rows of `vocab` logits x (dtype F16, BF16 or F32;
+ * element (b, t, i) at b*s_batch + t*s_token + i):
+ *   logp    = x[target] - ln sum_i exp(x_i), negated if `negate` is not 0
+ *   entropy = -sum_i p_i ln p_i in nats; NULL if not wanted
+ *   top_logp, top_ids: the `top` likeliest tokens in descending order, equal
+ *             logits by lower index; int32 ids; contiguous [batch][T][top];
+ *             0 <= top <= min(32, vocab) (top == 0: NULL)
+ * targets: device int64, element (b, t) at b*t_batch + t*t_token; a target of
+ * -1 (none) gives logp 0, another one outside [0, vocab) NaN.  logp and
+ * entropy: fp32, element (b, t) at b*o_batch + t*o_token; logp NULL (targets
+ * too then) if not wanted.
+ * batch * T below 2^24, vocab below 2^31.
+ * A row without a finite sum (a NaN or +inf logit, or every logit -inf) gives
+ * NaN, and ids of -1; semkv_rank reports the NaN.
+ * workspace: device, semkv_token_logprobs_workspace() bytes (0: may be NULL),
+ * needs no clearing. */
+int semkv_token_logprobs_workspace(int64_t rows, int64_t vocab, int32_t top, size_t* bytes);
+int semkv_token_logprobs(const void* logits, int32_t dtype, int32_t batch, int64_t T, int64_t vocab, int64_t s_batch,
+                         int64_t s_token, const int64_t* targets, int64_t t_batch, int64_t t_token, int32_t negate,
+                         float* logp, float* entropy, int64_t o_batch, int64_t o_token, int32_t top, float* top_logp,
+                         int32_t* top_ids, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,7 @@ from . import _abi
 from ._abi import BASE_AFFINE, BASE_ROT_AFFINE, BASE_TQ, SemKVError, check, lib
 
 __all__ = ["SemKVCache", "SemKVError", "BASE_AFFINE", "BASE_TQ", "BASE_ROT_AFFINE", "tq_codebook", "cache_sizes",
-           "score_hidden", "INDICATORS"]
+           "score_hidden", "INDICATORS", "PagedKV4", "make_paged_config", "paged_sizes", "token_logprobs", "score_tokens"]
 
 INDICATORS = {"delta_norm": _abi.IND_DELTA_NORM, "norm": _abi.IND_NORM, "variance": _abi.IND_VARIANCE,
               "cosine_delta": _abi.IND_COSINE_DELTA}
@@ -264,3 +264,6 @@ class SemKVCache:
             off += self.sz.cap_hi_tiles * self.sz.record_bytes_hi
         n = (self.sz.cap_hi_tiles if pool == 0 else self.sz.cap_lo_tiles) if n_tiles is None else n_tiles
         return self.pools[off:off + n * rb]
+
+
+from .paged import PagedKV4, make_paged_config, paged_sizes, score_tokens, token_logprobs  # noqa: E402

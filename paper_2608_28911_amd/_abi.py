@@ -11,9 +11,9 @@ vp = ctypes.c_void_p
 SEMKV_OK, SEMKV_EINVAL, SEMKV_EUNSUPPORTED, SEMKV_ECAPACITY, SEMKV_ENAN, SEMKV_EHIP, SEMKV_ESTATE = \
     0, -1, -2, -3, -4, -5, -6
 BASE_AFFINE, BASE_TQ, BASE_ROT_AFFINE = 0, 1, 2
-STATUS_NAN_SCORE, STATUS_NONFINITE_KV = 1, 2
+STATUS_NAN_SCORE, STATUS_NONFINITE_KV, STATUS_BAD_INDEX, STATUS_NO_PAGES = 1, 2, 4, 8
 IND_DELTA_NORM, IND_NORM, IND_VARIANCE, IND_COSINE_DELTA = 0, 1, 2, 3
-DTYPE_F16, DTYPE_BF16 = 0, 1
+DTYPE_F16, DTYPE_BF16, DTYPE_F32 = 0, 1, 2
 
 
 class Config(ctypes.Structure):
@@ -38,6 +38,21 @@ class Cache(ctypes.Structure):
                 ("n_prompt", i64), ("n_hi", i64), ("n_lo", i64), ("n_scored", i32), ("appended", u32 * 4)]
 
 
+class PagedConfig(ctypes.Structure):
+    _fields_ = [(n, i32) for n in ("n_layers", "n_kv_heads", "n_q_heads", "head_dim", "group", "n_pages", "max_seqs",
+                                   "seq_pages")]
+
+
+class PagedSizes(ctypes.Structure):
+    _fields_ = [(n, sz) for n in ("pool_bytes", "state_bytes", "workspace_bytes")] + \
+               [(n, i64) for n in ("record_bytes", "page_bytes", "lens_word", "table_word", "refs_word", "free_word",
+                                   "scratch_word")]
+
+
+class Paged(ctypes.Structure):
+    _fields_ = [("cfg", PagedConfig), ("sz", PagedSizes), ("pool", vp), ("state", vp), ("status", vp)]
+
+
 EXPORTS = {
     "semkv_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "semkv_cache_sizes": (ctypes.c_int, [ctypes.POINTER(Config), ctypes.POINTER(Sizes)]),
@@ -59,6 +74,19 @@ EXPORTS = {
     "semkv_dequant": (ctypes.c_int, [ctypes.POINTER(Cache), i32, vp, vp, vp]),
     "semkv_score_hidden": (ctypes.c_int, [i32, vp, i32, i32, i32, i64, i32, i64, i64, i64, vp, vp]),
     "semkv_score_kv_norm": (ctypes.c_int, [ctypes.POINTER(Cache), vp, i64, i64, i64, i64, i64, vp, vp]),
+    "semkv_paged_cache_sizes": (ctypes.c_int, [ctypes.POINTER(PagedConfig), ctypes.POINTER(PagedSizes)]),
+    "semkv_paged_init": (ctypes.c_int, [ctypes.POINTER(Paged), ctypes.POINTER(PagedConfig), vp, vp, vp, vp]),
+    "semkv_paged_assign": (ctypes.c_int, [ctypes.POINTER(Paged), vp, vp, vp]),
+    "semkv_paged_reserve": (ctypes.c_int, [ctypes.POINTER(Paged), vp, vp]),
+    "semkv_paged_fork": (ctypes.c_int, [ctypes.POINTER(Paged), vp, vp]),
+    "semkv_paged_compact": (ctypes.c_int, [ctypes.POINTER(Paged), vp, i64, vp, vp]),
+    "semkv_paged_write": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, vp, i32, i64, i64, i64, vp, i32, i64, vp]),
+    "semkv_paged_read": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, vp, i32, vp, i32, i64, vp]),
+    "semkv_paged_attn": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, i32, i64, i64, f32, vp, i32, i64, vp, vp, vp,
+                                        sz, vp]),
+    "semkv_token_logprobs_workspace": (ctypes.c_int, [i64, i64, i32, ctypes.POINTER(sz)]),
+    "semkv_token_logprobs": (ctypes.c_int, [vp, i32, i32, i64, i64, i64, i64, vp, i64, i64, i32, vp, vp, i64, i64, i32,
+                                            vp, vp, vp, sz, vp]),
 }
 
 _lib = None

@@ -27,6 +27,10 @@ SOURCES = {
     "quant.hip": ["-ffp-contract=off"],
     "decode.hip": ["-fconstexpr-steps=33554432"],   # the compile-time checks of the 7-level tables
     "score.hip": ["-ffp-contract=off"],
+    "paged.hip": ["-ffp-contract=off"],
+    "paged_attn.hip": [],
+    "paged_api.hip": [],
+    "logprob.hip": [],
 }
 
 

@@ -1,0 +1,673 @@
+// paged.hip -- the paged 4-bit cache on gfx950: quantizing rows into pages,
+// reading them back, and the calls on page tables (assign, reserve, fork,
+// compact).
+#include <hip/hip_fp16.h>
+
+#include "paged.h"
+
+namespace semkv {
+namespace {
+
+constexpr int kBad = 4, kNoPages = 8, kNonfinite = 2;   // status bits
+
+__device__ inline float h2f(uint32_t b) { return __half2float(__ushort_as_half(uint16_t(b))); }
+__device__ inline uint32_t f2h(float f) { return __half_as_ushort(__float2half_rn(f)); }
+
+// ---- page tables ---------------------------------------------------------
+
+__device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// Exclusive sum over the 1024 threads of the workgroup; `total` for all.
+__device__ inline int block_scan(int x, int* waves, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int incl = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(incl, d);
+    if (lane >= d) incl += up;
+  }
+  __syncthreads();                      // `waves` may still be read from an earlier call
+  if (lane == 63) waves[w] = incl;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int v = waves[i];
+    before += i < w ? v : 0;
+    total += v;
+  }
+  return before + incl - x;
+}
+
+// Takes the `want` lowest-numbered free pages into list[0 .. want): their bits
+// are cleared and their counts set to 1.  False, and nothing done, if there
+// are fewer.  Called by a whole 1024-thread workgroup; each thread owns a run
+// of bitmap words.
+__device__ inline bool take_pages(const PagedView& c, int want, int* waves) {
+  const int words = (c.n_pages + 31) / 32, per = (words + 1023) / 1024;
+  const int w0 = threadIdx.x * per, w1 = min(w0 + per, words);
+  int n = 0;
+  for (int w = w0; w < w1; ++w) n += __popc(c.free[w]);
+  int total;
+  int at = block_scan(n, waves, total);
+  if (total < want) return false;
+  for (int w = w0; w < w1 && at < want; ++w) {
+    uint32_t bits = c.free[w];
+    while (bits && at < want) {
+      const int p = 32 * w + __ffs(bits) - 1;
+      bits &= bits - 1;
+      c.list[at++] = p;
+      c.refs[p] = 1;
+    }
+    c.free[w] = bits;
+  }
+  return true;
+}
+
+// One slot more or less that holds page p.
+__device__ inline void hold(const PagedView& c, int p) { atomicAdd(c.refs + p, 1); }
+__device__ inline void release(const PagedView& c, int p) {
+  if (atomicSub(c.refs + p, 1) == 1) atomicOr(c.free + (p >> 5), 1u << (p & 31));
+}
+
+__global__ __launch_bounds__(256) void paged_clear_kernel(PagedView c) {
+  const int64_t i0 = int64_t(blockIdx.x) * 256 + threadIdx.x, step = int64_t(gridDim.x) * 256;
+  for (int64_t i = i0; i < int64_t(c.max_seqs) * c.seq_pages; i += step) c.table[i] = -1;
+  for (int64_t i = i0; i < c.n_pages; i += step) c.refs[i] = 0;
+  for (int64_t i = i0; i < c.max_seqs; i += step) {
+    c.lens[i] = 0;
+    c.cow[2 * i] = -1;
+  }
+  const int words = (c.n_pages + 31) / 32;
+  for (int64_t i = i0; i < words; i += step) {
+    const int left = c.n_pages - int(32 * i);
+    c.free[i] = left >= 32 ? ~0u : (1u << left) - 1u;
+  }
+  if (i0 == 0) *c.stalled = 0;
+}
+
+// The caller's tables over empty ones (paged_clear_kernel): entries in use are
+// copied and counted.
+__global__ __launch_bounds__(256) void paged_assign_kernel(PagedView c, const int32_t* lens, const int32_t* table) {
+  const int s = blockIdx.y, col = blockIdx.x * 256 + threadIdx.x;
+  const int given = lens[s], most = kPage * c.seq_pages;
+  const int len = min(max(given, 0), most);
+  if (col == 0) {
+    c.lens[s] = len;
+    if (len != given) atomicOr(c.status, kBad);
+  }
+  if (col >= div_up(len, kPage)) return;
+  const int64_t at = int64_t(s) * c.seq_pages + col;
+  const int p = table[at];
+  if (p < 0 || p >= c.n_pages) {
+    atomicOr(c.status, kBad);
+    return;
+  }
+  c.table[at] = p;
+  hold(c, p);
+  atomicAnd(c.free + (p >> 5), ~(1u << (p & 31)));
+}
+
+__global__ __launch_bounds__(1024) void paged_reserve_kernel(PagedView c, const int32_t* n_new) {
+  __shared__ int waves[16];
+  __shared__ int last_of[kMaxSeqs];     // shared last page that sequence s grows into, -1: none
+  __shared__ int base_of[kMaxSeqs + 1], held_of[kMaxSeqs];
+  __shared__ int full;
+  const int t = threadIdx.x;
+  const bool mine = t < c.max_seqs;
+  int len = 0, n = 0, last = -1, count = 0;
+  bool fits = true;
+  if (mine) {
+    len = c.lens[t];
+    n = n_new[t];
+    if (n < 0) {
+      atomicOr(c.status, kBad);
+      n = 0;
+    }
+    fits = n <= kPage * c.seq_pages - len;
+    if (fits && n > 0 && len % kPage != 0) {
+      last = c.table[int64_t(t) * c.seq_pages + len / kPage];
+      if (last >= 0) count = c.refs[last];
+    }
+  }
+  if (count < 2) last = -1;
+  last_of[t] = last;
+  if (t == 0) full = 0;
+  __syncthreads();
+  if (!fits) full = 1;
+  bool copy = false;
+  if (last >= 0) {                      // others hold it: all but the lowest if every one grows
+    int same = 0, lower = 0;
+    for (int s = 0; s < c.max_seqs; ++s) {
+      const int is = last_of[s] == last;
+      same += is;
+      lower += s < t ? is : 0;
+    }
+    copy = same != count || lower > 0;
+  }
+  __syncthreads();
+  const bool no_room = full != 0;
+  const int held = div_up(len, kPage), want = no_room ? 0 : div_up(len + n, kPage);
+  const int need = no_room ? 0 : want - held + copy;
+  int total;
+  const int base = block_scan(need, waves, total);
+  if (t < c.max_seqs) c.cow[2 * t] = -1;
+  if (no_room || !take_pages(c, total, waves)) {
+    if (t == 0) {
+      *c.stalled = 1;
+      atomicOr(c.status, kNoPages);
+    }
+    return;
+  }
+  base_of[t] = base;
+  held_of[t] = held - copy;             // the entry that the sequence's first page goes to
+  if (t == 0) {
+    base_of[kMaxSeqs] = total;
+    *c.stalled = 0;
+  }
+  __threadfence_block();
+  __syncthreads();
+  if (copy) {
+    c.cow[2 * t] = last;
+    c.cow[2 * t + 1] = c.list[base];
+    atomicSub(c.refs + last, 1);
+  }
+  for (int r = t; r < total; r += 1024) {
+    int lo = 0, hi = kMaxSeqs;          // the last sequence whose base is at most r
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (base_of[mid] <= r) lo = mid;
+      else hi = mid;
+    }
+    c.table[int64_t(lo) * c.seq_pages + held_of[lo] + (r - base_of[lo])] = c.list[r];
+  }
+  if (mine) c.lens[t] = len + n;
+}
+
+// The copies of shared last pages: 16 KB a workgroup.
+constexpr int kCopyVecs = 1024;
+__global__ __launch_bounds__(256) void paged_copy_kernel(PagedView c) {
+  const int s = blockIdx.y, src = c.cow[2 * s];
+  if (src < 0) return;
+  const int64_t bytes = int64_t(c.record) * c.n_layers * c.n_kv_heads, vecs = bytes / 16;
+  const uint4* from = reinterpret_cast<const uint4*>(c.pool + src * bytes);
+  uint4* to = reinterpret_cast<uint4*>(c.pool + c.cow[2 * s + 1] * bytes);
+  const int64_t i0 = int64_t(blockIdx.x) * kCopyVecs + threadIdx.x;
+  uint4 v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (i0 + 256 * k < vecs) v[k] = from[i0 + 256 * k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (i0 + 256 * k < vecs) to[i0 + 256 * k] = v[k];
+}
+
+// fork, first half: the new rows, and a count more for each page that a
+// changed slot takes over.  The second half (paged_install_kernel) counts down
+// what the slots held before, so no page is free in between.
+__global__ __launch_bounds__(256) void paged_fork_kernel(PagedView c, const int32_t* parent) {
+  const int s = blockIdx.y, col = blockIdx.x * 256 + threadIdx.x;
+  int p = parent[s];
+  const bool bad = p < -1 || p >= c.max_seqs;
+  if (bad) p = s;
+  if (col == 0) {
+    if (bad) atomicOr(c.status, kBad);
+    c.changed[s] = p != s;
+    c.new_lens[s] = p < 0 ? 0 : c.lens[p];
+  }
+  if (p == s || col >= c.seq_pages) return;
+  const int page = p < 0 ? -1 : c.table[int64_t(p) * c.seq_pages + col];
+  c.new_table[int64_t(s) * c.seq_pages + col] = page;
+  if (page >= 0) hold(c, page);
+}
+
+// The new rows of the changed slots; `listed`: row s is the run of `list` from
+// base[s] (compact), else new_table's row (fork).
+__global__ __launch_bounds__(256) void paged_install_kernel(PagedView c, int listed) {
+  const int s = blockIdx.y, col = blockIdx.x * 256 + threadIdx.x;
+  if (!c.changed[s] || col >= c.seq_pages) return;
+  const int64_t at = int64_t(s) * c.seq_pages + col;
+  const int len = c.new_lens[s], old = c.table[at];
+  int page;
+  if (listed) page = col < div_up(len, kPage) ? c.list[c.base[s] + col] : -1;
+  else page = c.new_table[at];
+  c.table[at] = page;
+  if (old >= 0) release(c, old);
+  if (col == 0) c.lens[s] = len;
+}
+
+// compact, first step: which slots change, and their fresh pages.
+__global__ __launch_bounds__(1024) void paged_plan_kernel(PagedView c, const int32_t* n_keep, int64_t ld) {
+  __shared__ int waves[16];
+  const int t = threadIdx.x;
+  int n = -1;
+  if (t < c.max_seqs) {
+    n = n_keep[t];
+    if (n < -1 || n > ld || n > int64_t(kPage) * c.seq_pages) {
+      atomicOr(c.status, kBad);
+      n = -1;
+    }
+  }
+  int total;
+  const int base = block_scan(n > 0 ? div_up(n, kPage) : 0, waves, total);
+  const bool ok = take_pages(c, total, waves);
+  if (!ok && t == 0) atomicOr(c.status, kNoPages);
+  if (t < c.max_seqs) {
+    c.changed[t] = ok && n >= 0;
+    c.new_lens[t] = n;
+    c.base[t] = base;
+  }
+}
+
+// compact, second step: one workgroup builds one record of a fresh page.  K: a
+// row is D/32 pieces' 16-byte lanes (D = 128; half lanes at D = 64), moved as
+// words.  V: a word holds 8 tokens of a channel; each nibble comes from its
+// own token's word.
+template <int D>
+__global__ __launch_bounds__(256) void paged_move_kernel(PagedView c, const int32_t* keep, int64_t ld) {
+  constexpr int KI = D / 32;                       // K words of a row and lane
+  __shared__ const uint8_t* rec_of[kPage];         // record of each kept token, null: none
+  __shared__ int slot_of[kPage];
+  const int s = blockIdx.y, tid = threadIdx.x;
+  const int layer = blockIdx.z / c.n_kv_heads, head = blockIdx.z % c.n_kv_heads;
+  if (!c.changed[s]) return;
+  const int n = c.new_lens[s], first = blockIdx.x * kPage;
+  if (first >= n) return;
+  if (tid < kPage) {
+    const uint8_t* rec = nullptr;
+    int slot = 0;
+    if (first + tid < n) {
+      const int pos = keep[s * ld + first + tid];
+      if (pos >= 0 && pos < c.lens[s]) {
+        const int p = c.table[int64_t(s) * c.seq_pages + pos / kPage];
+        if (p >= 0) rec = paged_record_at(c, p, layer, head);
+        slot = pos % kPage;
+      } else if (layer == 0 && head == 0) {
+        atomicOr(c.status, kBad);
+      }
+    }
+    rec_of[tid] = rec;
+    slot_of[tid] = slot;
+  }
+  __syncthreads();
+  uint8_t* out = paged_record_at(c, c.list[c.base[s] + blockIdx.x], layer, head);
+  constexpr int CB = paged_code_bytes(D);
+  uint32_t* ok = reinterpret_cast<uint32_t*>(out);
+  for (int i = tid; i < kPage * D / 8; i += 256) {      // word i of the destination: piece, lane, w
+    const int w = i & 3, lane = (i >> 2) & 63, x = 4 * (i >> 8) + w;
+    const int t = 16 * (x / KI) + (lane & 15), blk = x % KI;
+    const uint8_t* rec = rec_of[t];
+    uint32_t v = 0;
+    if (rec) {
+      const int st = slot_of[t], sx = (st / 16) * KI + blk;
+      v = reinterpret_cast<const uint32_t*>(rec)[((sx >> 2) * 64 + (lane & 48) + (st & 15)) * 4 + (sx & 3)];
+    }
+    ok[i] = v;
+  }
+  uint32_t* ov = reinterpret_cast<uint32_t*>(out + CB);
+  for (int i = tid; i < kPage * D / 8; i += 256) {
+    const int w = i & 3, lane = (i >> 2) & 63, x = 4 * (i >> 8) + w;
+    const int t0 = 32 * (x & 1) + 4 * (lane >> 4);
+    uint32_t v = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = t0 + 16 * (j >> 2) + (j & 3);
+      const uint8_t* rec = rec_of[t];
+      if (!rec) continue;
+      const int st = slot_of[t], sx = (x & ~1) | (st >> 5), sj = ((st >> 4) & 1) * 4 + (st & 3);
+      const uint32_t word = reinterpret_cast<const uint32_t*>(rec + CB)[((sx >> 2) * 64 + ((st >> 2) & 3) * 16 + (lane & 15)) * 4 + (sx & 3)];
+      const uint32_t nib = (word >> (4 * (sj >> 1) + 16 * (sj & 1))) & 15u;
+      v |= nib << (4 * (j >> 1) + 16 * (j & 1));
+    }
+    ov[i] = v;
+  }
+  // metadata: [K or V][group][token]
+  uint32_t* om = reinterpret_cast<uint32_t*>(out + 2 * CB);
+  const int groups = 2 * (D / c.group);
+  for (int i = tid; i < groups * kPage; i += 256) {
+    const int t = i & 63;
+    const uint8_t* rec = rec_of[t];
+    om[i] = rec ? reinterpret_cast<const uint32_t*>(rec + 2 * CB)[(i & ~63) + slot_of[t]] : 0u;
+  }
+}
+
+// ---- rows ----------------------------------------------------------------
+
+// Pages that the last `count` of `len` tokens touch.
+__device__ inline int pages_touched(int len, int count) {
+  const int first = max(len - count, 0);
+  return len > first ? (len - 1) / kPage - first / kPage + 1 : 0;
+}
+
+// What a workgroup of write or read works on: one page of one sequence.
+struct PageWork {
+  int seq;                      // -1: none
+  int page;                     // page id, -1: missing
+  int lo, hi;                   // slots of the page that are rows of the call
+  int64_t row0;                 // row of slot 0 (of slot lo: row0 + lo)
+};
+__device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int flat) {
+  PageWork k;
+  int tile;
+  const int lane = threadIdx.x & 63;
+  k.seq = find_tile(r.n_seqs, flat, lane,
+                    [&](int s) { return pages_touched(c.lens[s], seq_rows(r, s).count); }, tile);
+  k.page = -1;
+  k.lo = k.hi = 0;
+  k.row0 = 0;
+  if (k.seq < 0) return k;
+  const SeqRows m = seq_rows(r, k.seq);
+  const int len = c.lens[k.seq], first = max(len - m.count, 0);
+  const int col = first / kPage + tile;
+  k.page = c.table[int64_t(k.seq) * c.seq_pages + col];
+  k.lo = max(first - col * kPage, 0);
+  k.hi = min(len - col * kPage, kPage);
+  k.row0 = int64_t(m.first) + (int64_t(col) * kPage - (len - m.count));
+  return k;
+}
+
+// Workgroups in x for a call of n_rows rows: every touched page holds a row.
+int64_t touched_bound(const PagedRows& r) {
+  const int64_t by_pages = r.n_rows / kPage + 2 * int64_t(r.n_seqs);
+  return r.n_rows < by_pages ? r.n_rows : by_pages;
+}
+
+// Starts that are no partition of rows, or rows before the first token.
+__device__ inline void check_rows(const PagedView& c, const PagedRows& r) {
+  for (int s = threadIdx.x; s < r.n_seqs; s += blockDim.x) {
+    const int32_t a = r.starts[s], b = r.starts[s + 1];
+    if (a < 0 || b < a || b > r.n_rows || b - a > c.lens[s]) atomicOr(c.status, kBad);
+  }
+}
+
+// One workgroup quantizes the rows of one (page, layer, kv head).  Four lanes
+// own a token row, D/4 channels each, for K and then for V; the codes go to
+// LDS as bytes and come out as the words of the record's layout.  A page that
+// the rows fill only in part keeps its other rows: K words belong to one row,
+// V words hold 8 tokens and are merged with what is there.
+template <int D, int G, int BF>
+__global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
+  constexpr int Q = D / 4;                         // channels of a lane
+  constexpr int LG = G / Q > 1 ? G / Q : 1;        // lanes of a group
+  constexpr int GQ = Q / G > 1 ? Q / G : 1;        // groups of a lane
+  constexpr int CB = paged_code_bytes(D), KI = D / 32;
+  constexpr int PITCH = D + 4;
+  __shared__ __align__(16) uint8_t codes[kPage * PITCH];
+  const PagedView& c = a.c;
+  const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
+  const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
+  if (*c.stalled) return;
+  const PageWork w = page_work(c, a.r, blockIdx.x);
+  if (w.seq < 0) return;
+  if (w.page < 0 || c.refs[w.page] > 1) {
+    if (tid == 0) atomicOr(c.status, kBad);
+    return;
+  }
+  const bool mine = slot >= w.lo && slot < w.hi;
+  uint8_t* rec = paged_record_at(c, w.page, layer, head);
+  bool bad = false;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint16_t* X = kv ? a.V : a.K;
+    const uint16_t* src = X + int64_t(blockIdx.z) * a.sL + (w.row0 + (mine ? slot : w.lo)) * a.sT + head * a.sH + q * Q;
+    float x[Q];
+#pragma unroll
+    for (int i = 0; i < Q / 8; ++i) {
+      const uint4 v = reinterpret_cast<const uint4*>(src)[i];
+      const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BF) {
+          x[8 * i + 2 * e] = __uint_as_float(d[e] << 16);
+          x[8 * i + 2 * e + 1] = __uint_as_float(d[e] & 0xFFFF0000u);
+        } else {
+          x[8 * i + 2 * e] = h2f(d[e] & 0xFFFFu);
+          x[8 * i + 2 * e + 1] = h2f(d[e] >> 16);
+        }
+      }
+    }
+    uint32_t* meta = reinterpret_cast<uint32_t*>(rec + 2 * CB + kv * paged_meta_bytes(D, G));
+    if (kv) __syncthreads();                       // K's codes have been read
+#pragma unroll
+    for (int g = 0; g < GQ; ++g) {
+      constexpr int N = Q / GQ;
+      float mn = x[g * N], mx = mn, nan = 0.0f * mn;
+#pragma unroll
+      for (int i = 1; i < N; ++i) {
+        mn = fminf(mn, x[g * N + i]);
+        mx = fmaxf(mx, x[g * N + i]);
+        nan = fmaf(x[g * N + i], 0.0f, nan);       // 0, or NaN once a value is not finite
+      }
+#pragma unroll
+      for (int m = 1; m < LG; m <<= 1) {
+        mn = fminf(mn, __shfl_xor(mn, m));
+        mx = fmaxf(mx, __shfl_xor(mx, m));
+        nan += __shfl_xor(nan, m);
+      }
+      const bool finite = nan == 0.0f;
+      bad |= mine && !finite;
+      // zero and scale as fp16, saturated; codes against the stored pair
+      const uint32_t zb = f2h(fminf(fmaxf(mn, -65504.0f), 65504.0f) + 0.0f);
+      const float z = h2f(zb);
+      const uint32_t sb = f2h(fminf(fmaxf((mx - z) / 15.0f, 0.0f), 65504.0f));
+      const float sc = h2f(sb), inv = sc > 0.0f ? 1.0f / sc : 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        uint32_t pack = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float r = fminf(fmaxf(__builtin_rintf((x[g * N + i + e] - z) * inv), 0.0f), 15.0f);
+          pack |= uint32_t(r) << (8 * e);
+        }
+        *reinterpret_cast<uint32_t*>(codes + slot * PITCH + q * Q + g * N + i) = finite ? pack : 0u;
+      }
+      if (mine && (LG == 1 || q % LG == 0)) meta[((q * Q) / G + g) * kPage + slot] = finite ? sb | zb << 16 : 0u;
+    }
+    __syncthreads();
+    uint32_t* words = reinterpret_cast<uint32_t*>(rec + kv * CB);
+    const int first = w.lo, last = w.hi;
+    for (int i = tid; i < kPage * D / 8; i += 256) {
+      const int lane = (i >> 2) & 63, x4 = 4 * (i >> 8) + (i & 3);
+      if (kv == 0) {
+        const int t = 16 * (x4 / KI) + (lane & 15);
+        if (t < first || t >= last) continue;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(codes + t * PITCH + 32 * (x4 % KI) + 8 * (lane >> 4));
+        uint32_t v = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v |= ((p[j >> 2] >> (8 * (j & 3))) & 15u) << (4 * (j >> 1) + 16 * (j & 1));
+        words[i] = v;
+      } else {
+        const int ch = 16 * (x4 >> 1) + (lane & 15), t0 = 32 * (x4 & 1) + 4 * (lane >> 4);
+        uint32_t v = 0, mask = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = t0 + 16 * (j >> 2) + (j & 3), sh = 4 * (j >> 1) + 16 * (j & 1);
+          if (t >= first && t < last) {
+            v |= uint32_t(codes[t * PITCH + ch]) << sh;
+            mask |= 15u << sh;
+          }
+        }
+        if (mask == ~0u) words[i] = v;
+        else if (mask) words[i] = (words[i] & ~mask) | v;
+      }
+    }
+  }
+  if (bad) atomicOr(c.status, kNonfinite);
+}
+
+// One workgroup returns the rows of one (page, layer, kv head): the record
+// goes to LDS, four lanes take a token row.
+template <int DT>
+__device__ inline void store8(void* p, int64_t at, const float (&v)[8]) {
+  if constexpr (DT == 2) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+    o[0] = make_float4(v[0], v[1], v[2], v[3]);
+    o[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t b[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if constexpr (DT == 0) {
+          b[e] = f2h(v[2 * i + e]);
+        } else {                                   // finite: round to nearest even
+          const uint32_t u = __float_as_uint(v[2 * i + e]);
+          b[e] = (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+        }
+      }
+      w[i] = b[0] | b[1] << 16;
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Rows that would precede their sequence's first token: zeros.  Rare, so a
+// thread takes a whole sequence's.
+template <int D, int DT>
+__device__ inline void early_rows(const PagedReadArgs& a, int head) {
+  const float zeros[8] = {};
+  for (int s = threadIdx.x; s < a.r.n_seqs; s += blockDim.x) {
+    const SeqRows m = seq_rows(a.r, s);
+    for (int i = 0; i < m.count - a.c.lens[s]; ++i) {
+      const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + m.first + i) * a.c.n_kv_heads + head) * D;
+      for (int j = 0; j < D; j += 8) {
+        store8<DT>(a.K, at + j, zeros);
+        store8<DT>(a.V, at + j, zeros);
+      }
+    }
+  }
+}
+
+template <int D, int DT>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
+  constexpr int Q = D / 4, CB = paged_code_bytes(D), KI = D / 32;
+  __shared__ __align__(16) uint32_t rec[paged_record(D, 32) / 4];
+  const PagedView& c = a.c;
+  const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
+  const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
+  if (blockIdx.x == 0) {
+    if (blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
+    early_rows<D, DT>(a, head);
+  }
+  const PageWork w = page_work(c, a.r, blockIdx.x);
+  if (w.seq < 0) return;
+  if (w.page >= 0) {
+    const uint4* src = reinterpret_cast<const uint4*>(paged_record_at(c, w.page, layer, head));
+    for (int i = tid; i < c.record / 16; i += 256) reinterpret_cast<uint4*>(rec)[i] = src[i];
+  }
+  __syncthreads();
+  if (slot < w.lo || slot >= w.hi) return;
+  const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + w.row0 + slot) * c.n_kv_heads + head) * D + q * Q;
+  const int groups = D / c.group;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint32_t* words = rec + kv * CB / 4;
+    const uint32_t* meta = rec + 2 * CB / 4 + kv * groups * kPage;
+#pragma unroll
+    for (int i = 0; i < Q; i += 8) {
+      const int ch = q * Q + i;
+      const uint32_t m = w.page >= 0 ? meta[ch / c.group * kPage + slot] : 0u;
+      const float sc = h2f(m & 0xFFFFu), z = h2f(m >> 16);
+      float v[8];
+      if (kv == 0) {
+        const int x = (slot / 16) * KI + ch / 32;
+        const uint32_t word = w.page >= 0 ? words[((x >> 2) * 64 + ((ch & 31) >> 3) * 16 + (slot & 15)) * 4 + (x & 3)] : 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(float((word >> (4 * (j >> 1) + 16 * (j & 1))) & 15u), sc, z);
+      } else {
+        const int x = (ch / 16) * 2 + slot / 32, j = ((slot >> 4) & 1) * 4 + (slot & 3);
+        const int sh = 4 * (j >> 1) + 16 * (j & 1);
+        const uint32_t* p = words + ((x >> 2) * 64 + ((slot >> 2) & 3) * 16 + (ch & 15)) * 4 + (x & 3);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(float(w.page >= 0 ? (p[4 * e] >> sh) & 15u : 0u), sc, z);
+      }
+      store8<DT>(kv ? a.V : a.K, at + i, v);
+    }
+  }
+}
+
+inline int done() { return hipGetLastError() == hipSuccess ? 0 : -5; }
+
+inline dim3 table_grid(const PagedView& c) { return dim3(unsigned((c.seq_pages + 255) / 256), unsigned(c.max_seqs)); }
+
+}  // namespace
+
+int launch_paged_clear(const PagedView& c, hipStream_t s) {   // no sequence holds a token
+  int64_t n = int64_t(c.max_seqs) * c.seq_pages;
+  if (n < c.n_pages) n = c.n_pages;
+  const int64_t blocks = (n + 255) / 256;
+  hipLaunchKernelGGL(paged_clear_kernel, dim3(unsigned(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, c);
+  return done();
+}
+
+int launch_paged_assign(const PagedView& c, const int32_t* lens, const int32_t* table, hipStream_t s) {
+  const int st = launch_paged_clear(c, s);
+  if (st) return st;
+  hipLaunchKernelGGL(paged_assign_kernel, table_grid(c), dim3(256), 0, s, c, lens, table);
+  return done();
+}
+
+int launch_paged_reserve(const PagedView& c, const int32_t* n_new, hipStream_t s) {
+  hipLaunchKernelGGL(paged_reserve_kernel, dim3(1), dim3(1024), 0, s, c, n_new);
+  const int64_t vecs = int64_t(c.record) * c.n_layers * c.n_kv_heads / 16;
+  hipLaunchKernelGGL(paged_copy_kernel, dim3(unsigned((vecs + kCopyVecs - 1) / kCopyVecs), unsigned(c.max_seqs)), dim3(256), 0, s, c);
+  return done();
+}
+
+int launch_paged_fork(const PagedView& c, const int32_t* parent, hipStream_t s) {
+  hipLaunchKernelGGL(paged_fork_kernel, table_grid(c), dim3(256), 0, s, c, parent);
+  hipLaunchKernelGGL(paged_install_kernel, table_grid(c), dim3(256), 0, s, c, 0);
+  return done();
+}
+
+int launch_paged_compact(const PagedView& c, const int32_t* keep, int64_t ld, const int32_t* n_keep, hipStream_t s) {
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, c, n_keep, ld);
+  int64_t pages = (ld + kPage - 1) / kPage;
+  if (pages > c.seq_pages) pages = c.seq_pages;
+  if (pages > 0) {
+    const dim3 grid(unsigned(pages), unsigned(c.max_seqs), unsigned(c.n_layers * c.n_kv_heads));
+    if (c.dim == 128) hipLaunchKernelGGL((paged_move_kernel<128>), grid, dim3(256), 0, s, c, keep, ld);
+    else hipLaunchKernelGGL((paged_move_kernel<64>), grid, dim3(256), 0, s, c, keep, ld);
+  }
+  hipLaunchKernelGGL(paged_install_kernel, table_grid(c), dim3(256), 0, s, c, 1);
+  return done();
+}
+
+template <int D, int G>
+static void write_of(const PagedWriteArgs& a, dim3 grid, hipStream_t s) {
+  if (a.bf16) hipLaunchKernelGGL((paged_write_kernel<D, G, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_write_kernel<D, G, 0>), grid, dim3(256), 0, s, a);
+}
+
+int launch_paged_write(const PagedWriteArgs& a, hipStream_t s) {
+  const dim3 grid(unsigned(touched_bound(a.r)), unsigned(a.c.n_kv_heads), unsigned(a.layers));
+  if (a.c.dim == 128) {
+    if (a.c.group == 128) write_of<128, 128>(a, grid, s);
+    else if (a.c.group == 64) write_of<128, 64>(a, grid, s);
+    else write_of<128, 32>(a, grid, s);
+  } else {
+    if (a.c.group == 64) write_of<64, 64>(a, grid, s);
+    else write_of<64, 32>(a, grid, s);
+  }
+  return done();
+}
+
+template <int D>
+static void read_of(const PagedReadArgs& a, dim3 grid, hipStream_t s) {
+  if (a.dtype == 0) hipLaunchKernelGGL((paged_read_kernel<D, 0>), grid, dim3(256), 0, s, a);
+  else if (a.dtype == 1) hipLaunchKernelGGL((paged_read_kernel<D, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_read_kernel<D, 2>), grid, dim3(256), 0, s, a);
+}
+
+int launch_paged_read(const PagedReadArgs& a, hipStream_t s) {
+  const dim3 grid(unsigned(touched_bound(a.r)), unsigned(a.c.n_kv_heads), unsigned(a.layers));
+  if (a.c.dim == 128) read_of<128>(a, grid, s);
+  else read_of<64>(a, grid, s);
+  return done();
+}
+
+}  // namespace semkv

@@ -1,0 +1,503 @@
+// paged_attn.hip -- causal attention over the paged 4-bit cache on gfx950.
+//
+// Rows of one (sequence, kv head): row r is query head r mod gqa of the
+// sequence's row r div gqa.  A workgroup takes 16 NR rows and a run of the
+// sequence's pages, its waves one page (a record of 64 tokens) at a time.
+//
+// Both products run on v_mfma_f32_16x16x32_f16 with nothing dequantized:
+//   scores  C[16 tokens][16 rows] = codes . q,   x = s_t (c.q) + z_t (sum q)
+//   values  C[16 channels][16 rows] = codes . w, w = p_t s_t, and the zeros'
+//           share sum_t p_t z_t is kept apart in fp32
+// A code enters as the fp16 subnormal c 2^-24 (bits 0..3 of a half) or
+// c 2^-20 (bits 4..7): one AND (and a shift for two of four) makes a pair, and
+// the other operand carries the 1/16 of the second kind.  A lane's 16-byte
+// loads of a record are its operands as they are, and the scores' layout
+// (lane: row lane mod 16, tokens 4 (lane div 16) + i) is the values' operand
+// layout, since the words of V hold their tokens in that order: the weights go
+// from one product to the next in registers.
+//
+// Softmax: one pass with a running reference M per row.  It includes the
+// exponent of the largest V scale seen, so that w = 2^(x - M + 7) s_t lies
+// within fp16 whatever the scales; it is moved only when a record would pass
+// it by 2^6.  Scores, sums, the zeros' share and the accumulators are fp32;
+// w is rounded to fp16 (nearest), and the share that the rounding takes from
+// the middle of the codes' range (7.5) is given back through the zeros' sum,
+// which leaves an error relative to the values' spread within their group.
+#include <hip/hip_fp16.h>
+
+#include "paged.h"
+
+namespace semkv {
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;
+constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx9 family)
+constexpr float kHead = 7.0f;     // log2 of the largest weight at the reference
+constexpr float kLag = 6.0f;      // the reference may lag a record by this much
+
+// 8 codes of a word as fp16: slots 0, 1, 4, 5 as c 2^-24, slots 2, 3, 6, 7 as c 2^-20
+__device__ inline half8v codes8(uint32_t w) {
+  const uint32_t h = w >> 8;
+  const uint4 v = make_uint4(w & 0x000F000Fu, w & 0x00F000F0u, h & 0x000F000Fu, h & 0x00F000F0u);
+  return __builtin_bit_cast(half8v, v);
+}
+
+__device__ inline float lo16(uint32_t m) { return float(__builtin_bit_cast(half2v, m)[0]); }
+__device__ inline float hi16(uint32_t m) { return float(__builtin_bit_cast(half2v, m)[1]); }
+
+// over the four lanes of a row (16 apart)
+__device__ inline float row_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float row_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// LDS that only one wave uses: its lanes' earlier accesses before its later ones
+__device__ inline void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// What a workgroup works on.
+struct Tile {
+  int seq, len, row0, rows, first;   // sequence, its tokens, its first row of the call, rows of (token, head), first of them
+  int pages, splits;                 // pages the tile's last row sees, and workgroups that share them
+};
+
+template <int ROWS>
+__device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
+  Tile k;
+  int t;
+  k.seq = find_tile(a.r.n_seqs, flat, lane, [&](int s) { return (seq_rows(a.r, s).count * a.gqa + ROWS - 1) / ROWS; }, t);
+  if (k.seq < 0) return k;
+  const SeqRows m = seq_rows(a.r, k.seq);
+  k.len = a.c.lens[k.seq];
+  k.row0 = m.first;
+  k.rows = m.count * a.gqa;
+  // the last rows, which see the most, first
+  k.first = ((k.rows + ROWS - 1) / ROWS - 1 - t) * ROWS;
+  const int last = (min(k.first + ROWS, k.rows) - 1) / a.gqa;      // row of the call
+  const int seen = k.len - m.count + last + 1;
+  k.pages = seen > 0 ? (seen + kPage - 1) / kPage : 0;
+  // a split holds a page for each wave at least
+  k.splits = max(1, min(a.nsplit, (k.pages + kWaves - 1) / kWaves));
+  return k;
+}
+
+__device__ inline uint32_t pack_out(float x, float y, bool bf16) {
+  if (!bf16) return __builtin_bit_cast(uint32_t, half2v{_Float16(x), _Float16(y)});
+  uint32_t b[2] = {__float_as_uint(x), __float_as_uint(y)};
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    b[e] = (b[e] & 0x7FFFFFFFu) > 0x7F800000u ? 0x7FC0u : (b[e] + 0x7FFFu + ((b[e] >> 16) & 1u)) >> 16;
+  return b[0] | b[1] << 16;
+}
+
+// Partial of one split: each row's D sums, its M and l.
+template <int D>
+constexpr int partial_floats(int rows) { return rows * (D + 4); }
+
+template <int D, int G, int NR>
+__global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a) {
+  constexpr int NK = D / 32, NC = D / 16, NG = D / G, KG = G / 32, CG = G / 16, ROWS = 16 * NR;
+  constexpr int CB = paged_code_bytes(D), NP = D / 32;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
+  const PagedView& c = a.c;
+  const int head = blockIdx.x % c.n_kv_heads, flat = blockIdx.x / c.n_kv_heads, split = blockIdx.y;
+  const Tile tl = tile_of<ROWS>(a, flat, lane);
+  if (tl.seq < 0 || split >= tl.splits) return;
+
+  // the rows' queries as fp16 operands, each row scaled by a power of two so
+  // that its largest value lies in [2^14, 2^15); slots 2, 3, 6, 7 carry 1/16
+  half8v qf[NR][NK];
+  float qs[NR][NG], cf[NR];
+  int seen[NR];                                    // last token the row sees
+  const int m0 = tl.len - tl.rows / a.gqa;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int row = tl.first + 16 * r + n;
+    const bool valid = row < tl.rows;
+    const int i = (valid ? row : tl.first) / a.gqa, g = (valid ? row : tl.first) - i * a.gqa;
+    seen[r] = m0 + i;
+    const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.sT + int64_t(head * a.gqa + g) * a.sH + 8 * kg;
+    uint32_t d[4 * NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const uint4 v = *reinterpret_cast<const uint4*>(src + 32 * k);
+      d[4 * k] = valid ? v.x : 0u;
+      d[4 * k + 1] = valid ? v.y : 0u;
+      d[4 * k + 2] = valid ? v.z : 0u;
+      d[4 * k + 3] = valid ? v.w : 0u;
+    }
+    float x[NK][8], mx = 0.0f;
+    if (a.bf16) {
+#pragma unroll
+      for (int i = 0; i < 8 * NK; ++i) x[i >> 3][i & 7] = __uint_as_float(i & 1 ? d[i >> 1] & 0xFFFF0000u : d[i >> 1] << 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 * NK; ++i) x[i >> 3][i & 7] = i & 1 ? hi16(d[i >> 1]) : lo16(d[i >> 1]);
+    }
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[k][e]));
+    mx = row_max(mx);
+    const int ex = mx > 0.0f ? min(max(15 - __builtin_amdgcn_frexp_expf(mx), -100), 126) : 0;
+    cf[r] = __builtin_ldexpf(a.scale_log2e, 24 - ex);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) qs[r][j] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const _Float16 h = _Float16(__builtin_ldexpf(x[k][e], ex - (e & 2 ? 4 : 0)));
+        qf[r][k][e] = h;
+        qs[r][k / KG] += float(h) * (e & 2 ? 0x1p-20f : 0x1p-24f);
+      }
+#pragma unroll
+    for (int j = 0; j < NG; ++j) qs[r][j] = row_sum(qs[r][j]);
+  }
+
+  float4v o[NR][NC];
+  float M[NR], l[NR], az[NR][NG];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    M[r] = -INFINITY;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NG; ++j) az[r][j] = 0.0f;
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) o[r][ct] = float4v{0, 0, 0, 0};
+  }
+
+  // the tile's first row sees the least: pages up to here need no mask
+  const int all_see = m0 + tl.first / a.gqa;
+  const int p0 = int(int64_t(tl.pages) * split / tl.splits), p1 = int(int64_t(tl.pages) * (split + 1) / tl.splits);
+  const int32_t* table = c.table + int64_t(tl.seq) * c.seq_pages;
+  // A wave's next record is loaded piece by piece as soon as the current one's
+  // piece has been used; past its last page, and for a page that is missing,
+  // the descriptor's size is 0 and the loads return zeros.
+  auto page_at = [&](int p) { return p < p1 ? __builtin_amdgcn_readfirstlane(table[p]) : -1; };
+  auto record = [&](int page) {
+    return __builtin_amdgcn_make_buffer_rsrc(paged_record_at(c, max(page, 0), a.layer, head), 0,
+                                             page < 0 ? 0 : paged_record(D, G), kBufferWord3);
+  };
+  auto load = [&](const __amdgpu_buffer_rsrc_t& rs, int offset) {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + offset, 0, 0));
+  };
+  // Metadata goes through LDS, a region for each wave: 16 lanes share a token's
+  __shared__ __align__(16) uint4 sm_meta[kWaves][32 * NG];
+  constexpr int MV = (32 * NG + 63) / 64;          // 16-byte loads of it
+  uint4 kw[NP], vw[NP], mw[MV];
+  int page = page_at(p0 + wave), next = page_at(p0 + wave + kWaves);
+  {
+    const auto rs = record(page);
+#pragma unroll
+    for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
+  }
+  for (int p = p0 + wave; p < p1; p += kWaves) {
+    const auto rs = record(next);
+    const int have = page < 0 ? 0 : tl.len;        // tokens of a missing page are past the end
+    page = next;
+    next = page_at(p + 2 * kWaves);
+    // a lane holds 4 tokens of a group, first K's groups, then V's.  V's for
+    // tokens past the sequence's end, which may be anything, become 0; the
+    // largest V scale of the others enters the softmax's reference
+    uint32_t smax = 0;
+#pragma unroll
+    for (int i = 0; i < MV; ++i) {
+      const int at = 64 * i + lane, t = p * kPage + 4 * (at & 15);
+      uint32_t m[4] = {mw[i].x, mw[i].y, mw[i].z, mw[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (at >= 16 * NG) m[e] = t + e < have ? m[e] : 0u;
+        smax = max(smax, at >= 16 * NG && at < 32 * NG ? m[e] & 0xFFFFu : 0u);
+      }
+      if (32 * NG % 64 == 0 || at < 32 * NG) sm_meta[wave][at] = make_uint4(m[0], m[1], m[2], m[3]);
+    }
+    wave_order();
+    const uint4* kmeta = sm_meta[wave] + kg;       // [group][tile][4 tokens of kg]
+    const uint4* vmeta = kmeta + 16 * NG;
+
+    // scores
+    float4v x[NR][4];
+    const uint32_t* kd = reinterpret_cast<const uint32_t*>(kw);
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        float4v acc[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) acc[r] = float4v{0, 0, 0, 0};
+#pragma unroll
+        for (int k = j * KG; k < (j + 1) * KG; ++k) {
+          const half8v A = codes8(kd[tt * NK + k]);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, qf[r][k], acc[r], 0, 0, 0);
+        }
+        const uint4 mk = kmeta[j * 16 + tt * 4];
+        const uint32_t m[4] = {mk.x, mk.y, mk.z, mk.w};
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float s = lo16(m[e]), z = hi16(m[e]);
+            const float y = j == 0 ? z * qs[r][j] : fmaf(z, qs[r][j], x[r][tt][e]);
+            x[r][tt][e] = fmaf(s, acc[r][e], y);
+          }
+      }
+      if (NG > 1) __builtin_amdgcn_sched_barrier(0);   // else the metadata of every tile is read at once, and spilled
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
+#pragma unroll
+    for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
+    const int t0 = p * kPage + 4 * kg;             // the lane's first token
+    if (p * kPage + kPage - 1 > all_see || have == 0) {   // not every row sees every token
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[r][tt][e] = t0 + 16 * tt + e > min(seen[r], have - 1) ? -INFINITY : x[r][tt][e] * cf[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) x[r][tt] *= cf[r];
+    }
+
+    // the reference: row maximum plus the exponent of the record's largest V scale
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) smax = max(smax, uint32_t(__shfl_xor(int(smax), d)));
+    const float se = float(int(smax >> 10)) - 14.0f;
+    float ref[NR];
+    bool move = false;
+    float cand[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      float mx = x[r][0][0];
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[r][tt][e]);
+      cand[r] = row_max(mx) + se;
+      move |= cand[r] > M[r] + kLag;
+    }
+    if (__any(move)) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const float Mn = fmaxf(M[r], cand[r]);
+        const float f = M[r] == -INFINITY ? 0.0f : exp2_fast(M[r] - Mn);
+        M[r] = Mn;
+        l[r] *= f;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) az[r][j] *= f;
+#pragma unroll
+        for (int ct = 0; ct < NC; ++ct) o[r][ct] *= f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) ref[r] = M[r] == -INFINITY ? 0.0f : M[r] - kHead;
+
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[r][tt][e] = exp2_fast(x[r][tt][e] - ref[r]);
+          l[r] += x[r][tt][e];
+        }
+    const uint32_t* vd = reinterpret_cast<const uint32_t*>(vw);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      // the group's weights, and the zeros' share
+      half8v wf[NR][2];
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        const uint4 mv = vmeta[j * 16 + tt * 4];
+        const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float s = lo16(m[e]), mid = fmaf(7.5f, s, hi16(m[e])), ss = e & 2 ? s * 0.0625f : s;
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const _Float16 w = _Float16(x[r][tt][e] * ss);
+            wf[r][tt >> 1][4 * (tt & 1) + e] = w;
+            az[r][j] = fmaf(float(w), e & 2 ? -120.0f : -7.5f, fmaf(x[r][tt][e], mid, az[r][j]));
+          }
+        }
+      }
+      if (NG > 1) __builtin_amdgcn_sched_barrier(0);
+      // values
+#pragma unroll
+      for (int ct = j * CG; ct < (j + 1) * CG; ++ct)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const half8v A = codes8(vd[ct * 2 + st]);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) o[r][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, wf[r][st], o[r][ct], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
+    wave_order();                                  // the metadata has been read
+  }
+
+  // the waves' states merge in LDS, 16 rows at a time; then the tile's output,
+  // or the split's partial
+  constexpr int PITCH = D + 4;
+  __shared__ float sm_m[kWaves][ROWS], sm_l[kWaves][ROWS];
+  __shared__ __align__(16) float sm_o[kWaves][16][PITCH];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    l[r] = row_sum(l[r]);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) az[r][j] = row_sum(az[r][j]);
+    if (kg == 0) {
+      sm_m[wave][16 * r + n] = M[r];
+      sm_l[wave][16 * r + n] = l[r];
+    }
+  }
+  __syncthreads();
+  float* part = a.ws + ((int64_t(flat) * c.n_kv_heads + head) * a.nsplit + split) * partial_floats<D>(ROWS);
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    float Mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) Mx = fmaxf(Mx, sm_m[w][16 * r + n]);
+    const float f = M[r] == -INFINITY ? 0.0f : exp2_fast(M[r] - Mx);
+    // a row without a token keeps its NaN, if it has one, and zeros else
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct) {
+      float4v v = o[r][ct] * 0x1p24f + az[r][ct / CG];
+      if (M[r] != -INFINITY) v *= f;
+      *reinterpret_cast<float4v*>(&sm_o[wave][n][16 * ct + 4 * kg]) = v;
+    }
+    __syncthreads();
+    constexpr int LPR = D / 4;                     // threads of an output row
+#pragma unroll
+    for (int k = 0; k < 16 * LPR / (64 * kWaves); ++k) {
+      const int at = threadIdx.x + k * 64 * kWaves, rr = at / LPR, ch = at % LPR * 4;
+      float My = -INFINITY, L = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) My = fmaxf(My, sm_m[w][16 * r + rr]);
+      float4v v = float4v{0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = sm_m[w][16 * r + rr], lw = sm_l[w][16 * r + rr];
+        L += mw == -INFINITY ? lw : lw * exp2_fast(mw - My);
+        v += *reinterpret_cast<const float4v*>(&sm_o[w][rr][ch]);
+      }
+      if (tl.splits > 1) {
+        float* row = part + (16 * r + rr) * (D + 4);
+        *reinterpret_cast<float4v*>(row + ch) = v;
+        if (ch == 0) {
+          row[D] = My;
+          row[D + 1] = L;
+        }
+      } else {
+        const int rowi = tl.first + 16 * r + rr;
+        if (rowi >= tl.rows) continue;
+        const int i = rowi / a.gqa, g = rowi - i * a.gqa;
+        const int64_t at_row = int64_t(tl.row0 + i) * c.n_kv_heads * a.gqa + head * a.gqa + g;
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        v *= inv;
+        *reinterpret_cast<uint2*>(a.out + at_row * D + ch) =
+            make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
+        if (ch == 0 && a.lse) a.lse[at_row] = L == 0.0f ? -INFINITY : (My - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The splits of a tile joined: one workgroup per (tile, kv head, 16 rows).
+template <int D, int NR>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int ROWS = 16 * NR, LPR = D / 4;
+  const int lane = threadIdx.x & 63;
+  const PagedView& c = a.c;
+  const int head = blockIdx.x % c.n_kv_heads, flat = blockIdx.x / c.n_kv_heads;
+  const Tile tl = tile_of<ROWS>(a, flat, lane);
+  if (tl.seq < 0 || tl.splits < 2) return;
+  const float* unit = a.ws + (int64_t(flat) * c.n_kv_heads + head) * a.nsplit * partial_floats<D>(ROWS);
+  for (int at = threadIdx.x; at < 16 * LPR; at += 256) {
+    const int rr = 16 * blockIdx.y + at / LPR, ch = at % LPR * 4, rowi = tl.first + rr;
+    if (rowi >= tl.rows) continue;
+    float M = -INFINITY, L = 0.0f;
+    float4v v = float4v{0, 0, 0, 0};
+    for (int s = 0; s < tl.splits; ++s) M = fmaxf(M, unit[s * partial_floats<D>(ROWS) + rr * (D + 4) + D]);
+    for (int s = 0; s < tl.splits; ++s) {
+      const float* row = unit + s * partial_floats<D>(ROWS) + rr * (D + 4);
+      const float f = row[D] == -INFINITY ? 1.0f : exp2_fast(row[D] - M);    // nothing seen: zeros (or NaN)
+      L = fmaf(row[D + 1], f, L);
+      v += *reinterpret_cast<const float4v*>(row + ch) * f;
+    }
+    const int i = rowi / a.gqa, g = rowi - i * a.gqa;
+    const int64_t at_row = int64_t(tl.row0 + i) * c.n_kv_heads * a.gqa + head * a.gqa + g;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    v *= inv;
+    *reinterpret_cast<uint2*>(a.out + at_row * D + ch) =
+        make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
+    if (ch == 0 && a.lse) a.lse[at_row] = L == 0.0f ? -INFINITY : (M - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+  }
+}
+
+constexpr int kSlots = 1024;      // workgroups that splitting may make: 4 a compute unit
+
+template <int D, int G, int NR>
+int launch(PagedAttnArgs a, hipStream_t s) {
+  // tiles of the call: a whole tile's rows each, and one more a sequence
+  const int64_t tiles = a.r.n_rows * a.gqa / (16 * NR) + (a.r.n_seqs < a.r.n_rows ? a.r.n_seqs : a.r.n_rows);
+  const int64_t units = tiles * a.c.n_kv_heads;
+  if (units >= (int64_t(1) << 24)) return -2;      // a grid's threads are counted in 32 bits
+  int64_t ns = kSlots / units;
+  if (ns > a.c.seq_pages) ns = a.c.seq_pages;
+  if (ns < 1) ns = 1;
+  a.n_tiles = int(tiles);
+  a.nsplit = int(ns);
+  hipLaunchKernelGGL((paged_attn_kernel<D, G, NR>), dim3(unsigned(units), unsigned(ns)), dim3(64 * kWaves), 0, s, a);
+  if (ns > 1) hipLaunchKernelGGL((paged_merge_kernel<D, NR>), dim3(unsigned(units), NR), dim3(256), 0, s, a);
+  return hipGetLastError() == hipSuccess ? 0 : -5;
+}
+
+template <int D, int G>
+int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
+  const int64_t rows = (a.r.n_rows * a.gqa + a.r.n_seqs - 1) / a.r.n_seqs;   // of a sequence, on average
+  if (rows <= 16) return launch<D, G, 1>(a, s);
+  return launch<D, G, 2>(a, s);
+}
+
+}  // namespace
+
+// kSlots partials of the widest tile
+size_t paged_attn_workspace(int d) { return size_t(kSlots) * 32 * (d + 4) * 4; }
+
+int launch_paged_attn(PagedAttnArgs a, size_t ws_bytes, hipStream_t s) {
+  if (ws_bytes < paged_attn_workspace(a.c.dim)) return -1;
+  if (a.c.dim == 128) {
+    if (a.c.group == 128) return launch_rows<128, 128>(a, s);
+    if (a.c.group == 64) return launch_rows<128, 64>(a, s);
+    return launch_rows<128, 32>(a, s);
+  }
+  if (a.c.group == 64) return launch_rows<64, 64>(a, s);
+  return launch_rows<64, 32>(a, s);
+}
+
+}  // namespace semkv
