@@ -343,7 +343,8 @@ typedef struct semkv_paged_config {
  *         where none; refs_word: [n_pages] table entries that name the page;
  *         free_word: bit p%32 of word p/32 set iff page p is free; then
  *         scratch.  Readable by the caller; written by the calls only.
- *  workspace: scratch of semkv_paged_attn; needs no clearing. */
+ *  workspace: scratch of semkv_paged_attn, zero before its first use (every
+ *         call leaves its counters zero again). */
 typedef struct semkv_paged_sizes {
   size_t pool_bytes, state_bytes, workspace_bytes;
   int64_t record_bytes, page_bytes, lens_word, table_word, refs_word, free_word, scratch_word;

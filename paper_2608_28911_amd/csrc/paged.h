@@ -66,7 +66,7 @@ struct PagedAttnArgs {
   PagedRows r;
   const uint16_t* q;
   int64_t sT, sH;
-  int32_t layer, bf16, gqa, n_tiles, nsplit;
+  int32_t layer, bf16, gqa, target;
   float scale_log2e;
   uint16_t* out;
   float* lse;

@@ -17,9 +17,9 @@
 // from one product to the next in registers.
 //
 // Softmax: one pass with a running reference M per row.  It includes the
-// exponent of the largest V scale seen, so that w = 2^(x - M + 7) s_t lies
+// exponent of the largest V scale seen, so that w = 2^(x - M + 10) s_t lies
 // within fp16 whatever the scales; it is moved only when a record would pass
-// it by 2^6.  Scores, sums, the zeros' share and the accumulators are fp32;
+// it by 2^5.  Scores, sums, the zeros' share and the accumulators are fp32;
 // w is rounded to fp16 (nearest), and the share that the rounding takes from
 // the middle of the codes' range (7.5) is given back through the zeros' sum,
 // which leaves an error relative to the values' spread within their group.
@@ -34,10 +34,16 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
+// Workgroups of 4 waves that pages are shared out to (2 a compute unit).  Where
+// a tile is split, ceil(pages / chunk) is below twice pages / chunk: at most 2
+// kSlots partials, of which each tile's first also names its counter of
+// finished splits, each on a 256-byte line at the workspace's head.
+constexpr int kSlots = 512, kCounterStride = 64, kCounterWords = 2 * kSlots * kCounterStride;
 constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx9 family)
-constexpr float kHead = 7.0f;     // log2 of the largest weight at the reference
-constexpr float kLag = 6.0f;      // the reference may lag a record by this much
+// fp16 weights: 2^10 at the reference, which may lag a record by 2^5 (below
+// 65504), so that a weight (a sixteenth of it in every second slot) keeps its 11
+// bits down to 2^-20 of the largest
+constexpr float kHead = 10.0f, kLag = 5.0f;
 
 // 8 codes of a word as fp16: slots 0, 1, 4, 5 as c 2^-24, slots 2, 3, 6, 7 as c 2^-20
 __device__ inline half8v codes8(uint32_t w) {
@@ -68,29 +74,79 @@ __device__ inline void wave_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// What a workgroup works on.
+// What a workgroup works on: a tile of a sequence's rows, and a share of the
+// pages that it sees.
 struct Tile {
   int seq, len, row0, rows, first;   // sequence, its tokens, its first row of the call, rows of (token, head), first of them
-  int pages, splits;                 // pages the tile's last row sees, and workgroups that share them
+  int pages, splits, split;          // pages the tile's last row sees, workgroups that share them, this one's place
+  int part;                          // the tile's first partial and its counter
 };
 
-template <int ROWS>
+// The pages of a call are shared out by what the sequences really hold: each
+// workgroup takes `chunk` pages at most, the call's tiles times pages over the
+// workgroups wanted for a kv head (a.target), and a page for each wave at
+// least.  A workgroup finds its tile from its flat index by a prefix sum over
+// the sequences, 64 at a time.
+template <int ROWS, int NW>
 __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
+  struct Share { int tiles, pages; };
+  auto share = [&](int s) {
+    Share k = {0, 0};
+    if (s < a.r.n_seqs) {
+      k.tiles = (seq_rows(a.r, s).count * a.gqa + ROWS - 1) / ROWS;
+      k.pages = (a.c.lens[s] + kPage - 1) / kPage;
+    }
+    return k;
+  };
+  Share mine = share(lane);
+  int64_t work = 0;
+  for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
+    const Share k = s0 ? share(s0 + lane) : mine;
+    work += int64_t(k.tiles) * k.pages;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+  const int64_t even = (work + a.target - 1) / a.target;
+  const int chunk = int(min(max(even, int64_t(NW)), int64_t(1) << 30));
   Tile k;
-  int t;
-  k.seq = find_tile(a.r.n_seqs, flat, lane, [&](int s) { return (seq_rows(a.r, s).count * a.gqa + ROWS - 1) / ROWS; }, t);
+  k.seq = -1;
+  int before = 0, parts = 0;
+  for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
+    if (s0) mine = share(s0 + lane);
+    const int splits = mine.pages > chunk ? (mine.pages + chunk - 1) / chunk : 1;
+    const int n = mine.tiles * splits, held = splits > 1 ? n : 0;
+    int incl = n, pincl = held;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(incl, d), pup = __shfl_up(pincl, d);
+      if (lane >= d) {
+        incl += up;
+        pincl += pup;
+      }
+    }
+    const uint64_t above = __ballot(before + incl > flat);
+    if (above) {
+      const int l = __ffsll((unsigned long long)above) - 1;
+      const int at = flat - before - __builtin_amdgcn_readlane(incl - n, l), sp = __builtin_amdgcn_readlane(splits, l);
+      const int t = at / sp, tiles = __builtin_amdgcn_readlane(mine.tiles, l);
+      k.seq = s0 + l;
+      k.split = at - t * sp;
+      k.part = parts + __builtin_amdgcn_readlane(pincl - held, l) + t * sp;
+      k.first = (tiles - 1 - t) * ROWS;            // the last rows, which see the most, first
+      break;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+    parts += __builtin_amdgcn_readlane(pincl, 63);
+  }
   if (k.seq < 0) return k;
   const SeqRows m = seq_rows(a.r, k.seq);
   k.len = a.c.lens[k.seq];
   k.row0 = m.first;
   k.rows = m.count * a.gqa;
-  // the last rows, which see the most, first
-  k.first = ((k.rows + ROWS - 1) / ROWS - 1 - t) * ROWS;
   const int last = (min(k.first + ROWS, k.rows) - 1) / a.gqa;      // row of the call
   const int seen = k.len - m.count + last + 1;
   k.pages = seen > 0 ? (seen + kPage - 1) / kPage : 0;
-  // a split holds a page for each wave at least
-  k.splits = max(1, min(a.nsplit, (k.pages + kWaves - 1) / kWaves));
+  k.splits = max(1, (k.pages + chunk - 1) / chunk);
   return k;
 }
 
@@ -103,18 +159,32 @@ __device__ inline uint32_t pack_out(float x, float y, bool bf16) {
   return b[0] | b[1] << 16;
 }
 
+// A store that another XCD's workgroups see
+__device__ inline void store_far(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Four channels of an output row: sums v and l relative to the reference M.
+template <int D>
+__device__ inline void put_row(const PagedAttnArgs& a, const Tile& tl, int head, int row, int ch, float M, float L, float4v v) {
+  const int i = row / a.gqa, g = row - i * a.gqa;
+  const int64_t at = int64_t(tl.row0 + i) * a.c.n_kv_heads * a.gqa + head * a.gqa + g;
+  v *= L == 0.0f ? 0.0f : 1.0f / L;                // no token: zeros
+  *reinterpret_cast<uint2*>(a.out + at * D + ch) = make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
+  if (ch == 0 && a.lse) a.lse[at] = L == 0.0f ? -INFINITY : (M - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+}
+
 // Partial of one split: each row's D sums, its M and l.
 template <int D>
 constexpr int partial_floats(int rows) { return rows * (D + 4); }
 
-template <int D, int G, int NR>
-__global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a) {
+template <int D, int G, int NR, int NW>
+__global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int NK = D / 32, NC = D / 16, NG = D / G, KG = G / 32, CG = G / 16, ROWS = 16 * NR;
   constexpr int CB = paged_code_bytes(D), NP = D / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const PagedView& c = a.c;
-  const int head = blockIdx.x % c.n_kv_heads, flat = blockIdx.x / c.n_kv_heads, split = blockIdx.y;
-  const Tile tl = tile_of<ROWS>(a, flat, lane);
+  const int head = blockIdx.x % c.n_kv_heads;
+  const Tile tl = tile_of<ROWS, NW>(a, blockIdx.x / c.n_kv_heads, lane);
+  const int split = tl.split;
   if (tl.seq < 0 || split >= tl.splits) return;
 
   // the rows' queries as fp16 operands, each row scaled by a power of two so
@@ -196,10 +266,10 @@ __global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_at
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + offset, 0, 0));
   };
   // Metadata goes through LDS, a region for each wave: 16 lanes share a token's
-  __shared__ __align__(16) uint4 sm_meta[kWaves][32 * NG];
+  __shared__ __align__(16) uint4 sm_meta[NW][32 * NG];
   constexpr int MV = (32 * NG + 63) / 64;          // 16-byte loads of it
   uint4 kw[NP], vw[NP], mw[MV];
-  int page = page_at(p0 + wave), next = page_at(p0 + wave + kWaves);
+  int page = page_at(p0 + wave), next = page_at(p0 + wave + NW);
   {
     const auto rs = record(page);
 #pragma unroll
@@ -209,11 +279,11 @@ __global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_at
 #pragma unroll
     for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
   }
-  for (int p = p0 + wave; p < p1; p += kWaves) {
+  for (int p = p0 + wave; p < p1; p += NW) {
     const auto rs = record(next);
     const int have = page < 0 ? 0 : tl.len;        // tokens of a missing page are past the end
     page = next;
-    next = page_at(p + 2 * kWaves);
+    next = page_at(p + 2 * NW);
     // a lane holds 4 tokens of a group, first K's groups, then V's.  V's for
     // tokens past the sequence's end, which may be anything, become 0; the
     // largest V scale of the others enters the softmax's reference
@@ -361,9 +431,9 @@ __global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_at
 
   // the waves' states merge in LDS, 16 rows at a time; then the tile's output,
   // or the split's partial
-  constexpr int PITCH = D + 4;
-  __shared__ float sm_m[kWaves][ROWS], sm_l[kWaves][ROWS];
-  __shared__ __align__(16) float sm_o[kWaves][16][PITCH];
+  constexpr int PITCH = D + 4, LPR = D / 4, NT = 64 * NW;   // LPR: threads of an output row
+  __shared__ float sm_m[NW][ROWS], sm_l[NW][ROWS];
+  __shared__ __align__(16) float sm_o[NW][16][PITCH];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     l[r] = row_sum(l[r]);
@@ -375,119 +445,162 @@ __global__ __launch_bounds__(64 * kWaves, D / G * NR >= 4 ? 1 : 2) void paged_at
     }
   }
   __syncthreads();
-  float* part = a.ws + ((int64_t(flat) * c.n_kv_heads + head) * a.nsplit + split) * partial_floats<D>(ROWS);
+  const int64_t unit = int64_t(head) * 2 * a.target + tl.part;     // partials of a kv head: below 2 target
+  float* parts = a.ws + kCounterWords + unit * partial_floats<D>(ROWS);
+  const int rows = min(tl.rows - tl.first, ROWS);
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
+    if (16 * r >= rows) break;
     float Mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) Mx = fmaxf(Mx, sm_m[w][16 * r + n]);
-    const float f = M[r] == -INFINITY ? 0.0f : exp2_fast(M[r] - Mx);
+    for (int w = 0; w < NW; ++w) Mx = fmaxf(Mx, sm_m[w][16 * r + n]);
     // a row without a token keeps its NaN, if it has one, and zeros else
+    const float f = M[r] == -INFINITY ? 1.0f : exp2_fast(M[r] - Mx);
+    if (16 * r + n < rows) {
 #pragma unroll
-    for (int ct = 0; ct < NC; ++ct) {
-      float4v v = o[r][ct] * 0x1p24f + az[r][ct / CG];
-      if (M[r] != -INFINITY) v *= f;
-      *reinterpret_cast<float4v*>(&sm_o[wave][n][16 * ct + 4 * kg]) = v;
+      for (int ct = 0; ct < NC; ++ct)
+        *reinterpret_cast<float4v*>(&sm_o[wave][n][16 * ct + 4 * kg]) = (o[r][ct] * 0x1p24f + az[r][ct / CG]) * f;
     }
     __syncthreads();
-    constexpr int LPR = D / 4;                     // threads of an output row
-#pragma unroll
-    for (int k = 0; k < 16 * LPR / (64 * kWaves); ++k) {
-      const int at = threadIdx.x + k * 64 * kWaves, rr = at / LPR, ch = at % LPR * 4;
+    for (int at = threadIdx.x; at < min(rows - 16 * r, 16) * LPR; at += NT) {
+      const int rr = at / LPR, ch = at % LPR * 4;
       float My = -INFINITY, L = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) My = fmaxf(My, sm_m[w][16 * r + rr]);
+      for (int w = 0; w < NW; ++w) My = fmaxf(My, sm_m[w][16 * r + rr]);
       float4v v = float4v{0, 0, 0, 0};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < NW; ++w) {
         const float mw = sm_m[w][16 * r + rr], lw = sm_l[w][16 * r + rr];
         L += mw == -INFINITY ? lw : lw * exp2_fast(mw - My);
         v += *reinterpret_cast<const float4v*>(&sm_o[w][rr][ch]);
       }
       if (tl.splits > 1) {
-        float* row = part + (16 * r + rr) * (D + 4);
-        *reinterpret_cast<float4v*>(row + ch) = v;
+        float* row = parts + split * partial_floats<D>(ROWS) + (16 * r + rr) * (D + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_far(row + ch + e, v[e]);
         if (ch == 0) {
-          row[D] = My;
-          row[D + 1] = L;
+          store_far(row + D, My);
+          store_far(row + D + 1, L);
         }
       } else {
-        const int rowi = tl.first + 16 * r + rr;
-        if (rowi >= tl.rows) continue;
-        const int i = rowi / a.gqa, g = rowi - i * a.gqa;
-        const int64_t at_row = int64_t(tl.row0 + i) * c.n_kv_heads * a.gqa + head * a.gqa + g;
-        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-        v *= inv;
-        *reinterpret_cast<uint2*>(a.out + at_row * D + ch) =
-            make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
-        if (ch == 0 && a.lse) a.lse[at_row] = L == 0.0f ? -INFINITY : (My - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+        put_row<D>(a, tl, head, tl.first + 16 * r + rr, ch, My, L, v);
       }
     }
     __syncthreads();
   }
-}
+  if (tl.splits < 2) return;
 
-// The splits of a tile joined: one workgroup per (tile, kv head, 16 rows).
-template <int D, int NR>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  constexpr int ROWS = 16 * NR, LPR = D / 4;
-  const int lane = threadIdx.x & 63;
-  const PagedView& c = a.c;
-  const int head = blockIdx.x % c.n_kv_heads, flat = blockIdx.x / c.n_kv_heads;
-  const Tile tl = tile_of<ROWS>(a, flat, lane);
-  if (tl.seq < 0 || tl.splits < 2) return;
-  const float* unit = a.ws + (int64_t(flat) * c.n_kv_heads + head) * a.nsplit * partial_floats<D>(ROWS);
-  for (int at = threadIdx.x; at < 16 * LPR; at += 256) {
-    const int rr = 16 * blockIdx.y + at / LPR, ch = at % LPR * 4, rowi = tl.first + rr;
-    if (rowi >= tl.rows) continue;
-    float M = -INFINITY, L = 0.0f;
+  // The last workgroup of the tile to arrive joins the splits.  Partials cross
+  // XCDs, whose L2s are apart: they are stored and loaded past them, and every
+  // thread's stores are complete before its workgroup is counted.
+  __shared__ int sm_last;
+  __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t* counter = reinterpret_cast<uint32_t*>(a.ws) + unit * kCounterStride;
+    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sm_last = before + 1 == uint32_t(tl.splits);
+    if (sm_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!sm_last) return;
+  __asm__ volatile("" ::: "memory");
+  // NT/LPR rows at once: where there are fewer, the rest share a row's splits
+  const int lanes = rows >= NT / LPR ? 1 : NT / LPR / rows;       // threads to a (row, 4 channels)
+  const int at0 = threadIdx.x / LPR, ch = threadIdx.x % LPR * 4, part0 = at0 % lanes;
+  constexpr int kFar = 16;                                        // cache policy sc1, as agent-scope loads
+  const auto far = __builtin_amdgcn_make_buffer_rsrc(parts, 0, tl.splits * partial_floats<D>(ROWS) * 4, kBufferWord3);
+  float* sm_j = &sm_o[0][0][0];                                   // [row][lane of it][D + 4]
+  static_assert(NT / LPR * (D + 4) <= NW * 16 * PITCH, "join scratch");
+  for (int row0 = 0; row0 < rows; row0 += NT / LPR) {
+    const int rr = row0 + at0 / lanes;
+    const bool mine = rr < rows;
+    constexpr int B = 8;                                          // splits in flight
+    float My = -INFINITY, L = 0.0f;
     float4v v = float4v{0, 0, 0, 0};
-    for (int s = 0; s < tl.splits; ++s) M = fmaxf(M, unit[s * partial_floats<D>(ROWS) + rr * (D + 4) + D]);
-    for (int s = 0; s < tl.splits; ++s) {
-      const float* row = unit + s * partial_floats<D>(ROWS) + rr * (D + 4);
-      const float f = row[D] == -INFINITY ? 1.0f : exp2_fast(row[D] - M);    // nothing seen: zeros (or NaN)
-      L = fmaf(row[D + 1], f, L);
-      v += *reinterpret_cast<const float4v*>(row + ch) * f;
+    for (int s0 = part0; mine && s0 < tl.splits; s0 += lanes * B) {
+      float m[B], ls[B];
+      float4v x[B];
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        // past the last split: the last again, with no weight
+        const int off = (min(s0 + k * lanes, tl.splits - 1) * partial_floats<D>(ROWS) + rr * (D + 4)) * 4;
+        const auto ml = __builtin_amdgcn_raw_buffer_load_b64(far, off + D * 4, 0, kFar);
+        m[k] = __uint_as_float(ml[0]);
+        ls[k] = __uint_as_float(ml[1]);
+        x[k] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(far, off + ch * 4, 0, kFar));
+      }
+      float Mn = My;
+#pragma unroll
+      for (int k = 0; k < B; ++k) Mn = fmaxf(Mn, m[k]);
+      const float keep = My == -INFINITY ? 1.0f : exp2_fast(My - Mn);
+      L *= keep;
+      v *= keep;
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        if (s0 + k * lanes >= tl.splits) continue;
+        const float f = m[k] == -INFINITY ? 1.0f : exp2_fast(m[k] - Mn);   // nothing seen: zeros (or NaN)
+        L = fmaf(ls[k], f, L);
+        v += x[k] * f;
+      }
+      My = Mn;
     }
-    const int i = rowi / a.gqa, g = rowi - i * a.gqa;
-    const int64_t at_row = int64_t(tl.row0 + i) * c.n_kv_heads * a.gqa + head * a.gqa + g;
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    v *= inv;
-    *reinterpret_cast<uint2*>(a.out + at_row * D + ch) =
-        make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
-    if (ch == 0 && a.lse) a.lse[at_row] = L == 0.0f ? -INFINITY : (M - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+    if (lanes > 1) {
+      __syncthreads();
+      float* j = sm_j + at0 * (D + 4);
+      *reinterpret_cast<float4v*>(j + ch) = v;
+      if (ch == 0) {
+        j[D] = My;
+        j[D + 1] = L;
+      }
+      __syncthreads();
+      if (part0 != 0 || !mine) continue;
+      float Mn = My;
+      for (int k = 1; k < lanes; ++k) Mn = fmaxf(Mn, j[k * (D + 4) + D]);
+      const float keep = My == -INFINITY ? 1.0f : exp2_fast(My - Mn);
+      L *= keep;
+      v *= keep;
+      for (int k = 1; k < lanes; ++k) {
+        const float mk = j[k * (D + 4) + D], f = mk == -INFINITY ? 1.0f : exp2_fast(mk - Mn);
+        L = fmaf(j[k * (D + 4) + D + 1], f, L);
+        v += *reinterpret_cast<const float4v*>(j + k * (D + 4) + ch) * f;
+      }
+      My = Mn;
+    }
+    if (mine) put_row<D>(a, tl, head, tl.first + rr, ch, My, L, v);
   }
 }
 
-constexpr int kSlots = 1024;      // workgroups that splitting may make: 4 a compute unit
-
-template <int D, int G, int NR>
+template <int D, int G, int NR, int NW>
 int launch(PagedAttnArgs a, hipStream_t s) {
   // tiles of the call: a whole tile's rows each, and one more a sequence
-  const int64_t tiles = a.r.n_rows * a.gqa / (16 * NR) + (a.r.n_seqs < a.r.n_rows ? a.r.n_seqs : a.r.n_rows);
+  const int64_t whole = a.r.n_rows * ((a.gqa + 16 * NR - 1) / (16 * NR));
+  int64_t tiles = a.r.n_rows * a.gqa / (16 * NR) + a.r.n_seqs;
+  if (tiles > whole) tiles = whole;
   const int64_t units = tiles * a.c.n_kv_heads;
-  if (units >= (int64_t(1) << 24)) return -2;      // a grid's threads are counted in 32 bits
-  int64_t ns = kSlots / units;
-  if (ns > a.c.seq_pages) ns = a.c.seq_pages;
-  if (ns < 1) ns = 1;
-  a.n_tiles = int(tiles);
-  a.nsplit = int(ns);
-  hipLaunchKernelGGL((paged_attn_kernel<D, G, NR>), dim3(unsigned(units), unsigned(ns)), dim3(64 * kWaves), 0, s, a);
-  if (ns > 1) hipLaunchKernelGGL((paged_merge_kernel<D, NR>), dim3(unsigned(units), NR), dim3(256), 0, s, a);
+  if (units >= (int64_t(1) << 22)) return -2;      // a grid's threads are counted in 32 bits
+  int64_t wanted = kSlots * 4 / NW / a.c.n_kv_heads;
+  if (wanted < 1) wanted = 1;
+  a.target = int(wanted);
+  // every tile, and a share of the wanted ones where pages are split; no more
+  // than a page a workgroup
+  int64_t grid = tiles + wanted;
+  if (a.c.seq_pages <= NW) grid = tiles;
+  hipLaunchKernelGGL((paged_attn_kernel<D, G, NR, NW>), dim3(unsigned(grid * a.c.n_kv_heads)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
 template <int D, int G>
 int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t rows = (a.r.n_rows * a.gqa + a.r.n_seqs - 1) / a.r.n_seqs;   // of a sequence, on average
-  if (rows <= 16) return launch<D, G, 1>(a, s);
-  return launch<D, G, 2>(a, s);
+  if (rows <= 16) return launch<D, G, 1, 8>(a, s);
+  return launch<D, G, 2, 4>(a, s);
 }
 
 }  // namespace
 
-// kSlots partials of the widest tile
-size_t paged_attn_workspace(int d) { return size_t(kSlots) * 32 * (d + 4) * 4; }
+// counters, and kSlots partials of the widest tile
+size_t paged_attn_workspace(int d) { return size_t(kCounterWords + 2 * kSlots * 32 * (d + 4)) * 4; }
 
 int launch_paged_attn(PagedAttnArgs a, size_t ws_bytes, hipStream_t s) {
   if (ws_bytes < paged_attn_workspace(a.c.dim)) return -1;

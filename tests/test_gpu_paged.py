@@ -557,7 +557,7 @@ def test_two_calls_at_once_with_a_workspace_each():
     c = make(n_pages=200, seqs=1, seq_pages=200)
     fill(c, [12000], rng)
     q = [rows(rng, (1, 8, 128), torch.float16) for _ in range(2)]
-    ws = [torch.empty_like(c.ws) for _ in range(2)]
+    ws = [torch.zeros_like(c.ws) for _ in range(2)]
     st = starts_of([1])
     want = [c.attn(0, x, st).clone() for x in q]
     torch.cuda.synchronize()
