@@ -100,15 +100,27 @@ __device__ inline void keep(Kept& s, uint32_t h, uint32_t l, int lane) {   // h,
     s.lo = ul;
   }
 }
-// Lanes flagged in `who` hold keys that may belong to the kept ones.
-__device__ inline void keep_all(Kept& s, uint64_t who, uint32_t h, uint32_t l, int k, int lane) {
-  while (who) {
-    const int from = __ffsll((unsigned long long)who) - 1;
-    who &= who - 1;
-    const uint32_t vh = __builtin_amdgcn_readlane(h, from), vl = __builtin_amdgcn_readlane(l, from);
+// The keys of lanes with `may` into the kept ones.  Those that no longer beat
+// the last kept one drop out at every insertion.
+__device__ inline void keep_all(Kept& s, bool may, uint32_t h, uint32_t l, int k, int lane) {
+  while (true) {
     const uint32_t th = __builtin_amdgcn_readlane(s.hi, k - 1), tlo = __builtin_amdgcn_readlane(s.lo, k - 1);
-    if (vh > th || (vh == th && vl > tlo)) keep(s, vh, vl, lane);
+    const uint64_t who = __ballot(may && (h > th || (h == th && l > tlo)));
+    if (!who) return;
+    const int from = __ffsll((unsigned long long)who) - 1;
+    keep(s, __builtin_amdgcn_readlane(h, from), __builtin_amdgcn_readlane(l, from), lane);
+    may = may && lane != from;
   }
+}
+
+// The k-th largest of the lanes' orders (its upper 24 bits): as many lanes hold
+// a logit that is no smaller, so a row's k likeliest are not below it.
+__device__ inline uint32_t kth_order(uint32_t h, int k) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int b = 31; b >= 8; --b)
+    if (__popcll(__ballot(h >= (t | 1u << b))) >= k) t |= 1u << b;
+  return t;
 }
 
 // Partial of one split of a row: m, S, T, then the kept keys.
@@ -174,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
     if (valid) add(s, e);
     if constexpr (TOP) {
       const uint32_t h = valid ? order_of(e) : 0u;
-      keep_all(kept, __ballot(valid && h >= last), h, ~uint32_t(i), k, lane);
+      keep_all(kept, valid, h, ~uint32_t(i), k, lane);
       last = __builtin_amdgcn_readlane(kept.hi, k - 1);
     }
   };
@@ -190,32 +202,41 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
       const int64_t at = v + lane + u * NT;
       if (at < v1) w[u] = xv[at];
     }
+    float e[U][V], mx[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = v + lane + u * NT;
-      const bool valid = at < v1;
-      float e[V];
-      unpack<DT>(w[u], e);
-      float mx = valid ? e[0] : -INFINITY;
+      const bool valid = v + lane + u * NT < v1;
+      unpack<DT>(w[u], e[u]);
+      mx[u] = -INFINITY;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (!valid) e[i] = -INFINITY;
-        mx = fmaxf(mx, e[i]);
+        if (!valid) e[u][i] = -INFINITY;
+        mx[u] = fmaxf(mx[u], e[u][i]);
       }
-      const float m = fmaxf(mx, s.m);
+      const float m = fmaxf(mx[u], s.m);
       if (m > s.m) raise(s, m);
 #pragma unroll
-      for (int i = 0; i < V; ++i) add(s, e[i]);
-      if constexpr (TOP) {
-        // a NaN row is reported by its sum: what is kept of it does not matter
-        if (__any(valid && order_of(mx) > last)) {
+      for (int i = 0; i < V; ++i) add(s, e[u][i]);
+    }
+    if constexpr (TOP) {
+      // a row with a NaN is reported by its sum: what is kept of it does not matter
+      uint32_t most = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) most = max(most, v + lane + u * NT < v1 ? order_of(mx[u]) : 0u);
+      if (__any(most > last)) {
+        // while the list fills, the lanes' maxima bound what it can end with
+        const uint32_t least = max(last, kth_order(most, k));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t at = v + lane + u * NT;
+          if (!__any(at < v1 && order_of(mx[u]) >= least)) continue;
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const uint32_t h = order_of(e[i]);
-            keep_all(kept, __ballot(valid && h >= last), h, ~uint32_t(head + at * V + i), k, lane);
+            const uint32_t h = order_of(e[u][i]);
+            keep_all(kept, at < v1 && h >= least, h, ~uint32_t(head + at * V + i), k, lane);
           }
-          last = __builtin_amdgcn_readlane(kept.hi, k - 1);
         }
+        last = __builtin_amdgcn_readlane(kept.hi, k - 1);
       }
     }
   }
@@ -239,7 +260,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
     for (int i = k; i < WAVES * k; i += 64) {              // the other waves' keys into wave 0's
       const bool valid = i + lane < WAVES * k;
       const uint32_t h = valid ? sm_hi[i + lane] : 0u, l = valid ? sm_lo[i + lane] : 0u;
-      keep_all(kept, __ballot(valid && h >= __builtin_amdgcn_readlane(kept.hi, k - 1)), h, l, k, lane);
+      keep_all(kept, valid, h, l, k, lane);
     }
   }
   if (a.nsplit > 1) {
@@ -279,7 +300,7 @@ __global__ __launch_bounds__(64) void token_merge_kernel(TokenArgs a) {
     const bool valid = at < a.nsplit * k;
     const uint32_t* q = p + sp * partial_words(k) + 4 + 2 * j;
     const uint32_t h = valid ? q[0] : 0u, l = valid ? q[1] : 0u;
-    keep_all(kept, __ballot(valid && h >= __builtin_amdgcn_readlane(kept.hi, k - 1)), h, l, k, lane);
+    keep_all(kept, valid, h, l, k, lane);
   }
   if (lane < k) finish_top(a, row, s, kept.hi, kept.lo, lane);
 }
