@@ -115,7 +115,7 @@ def bound(abi, monkeypatch):
     import torch
     import paper_2608_28911_amd as P
     from paper_2608_28911_amd import paged
-    monkeypatch.setattr(P, "_stream", lambda: 0)
+    monkeypatch.setattr(paged, "_enqueue", lambda index, f, what, *args: f(*args, 0))
     real, rec = abi.lib(), Recorder()
 
     class Lib:
@@ -141,7 +141,7 @@ def test_binding_checks_what_it_is_given(bound):
         lambda: c.write(0, kv, kv.transpose(0, 1).contiguous().transpose(0, 1), i(3)),
         lambda: c.read(0, i(3), 5, dtype=torch.float64), lambda: c.read(0, i(3), 5, out=(kv, kv[:4])),
         lambda: c.attn(0, q[:, :31], i(3)), lambda: c.attn(0, q.float(), i(3)), lambda: c.attn(0, q, i(3), out=q.bfloat16()),
-        lambda: c.attn(0, q, i(3), lse=torch.zeros((5, 31))), lambda: c.attn(0, q, i(3).to("meta")),
+        lambda: c.attn(0, q, i(3), lse=torch.zeros((5, 31))), lambda: c.attn(0, q, i(3).long()),
     ]
     for k, call in enumerate(bad):
         with pytest.raises(ValueError):
