@@ -107,7 +107,7 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
   const int64_t even = (work + a.target - 1) / a.target;
-  const int chunk = int(min(max(even, int64_t(NW)), int64_t(1) << 30));
+  const int chunk = __builtin_amdgcn_readfirstlane(int(min(max(even, int64_t(NW)), int64_t(1) << 30)));
   Tile k;
   k.seq = -1;
   int before = 0, parts = 0;
@@ -139,8 +139,11 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
     parts += __builtin_amdgcn_readlane(pincl, 63);
   }
   if (k.seq < 0) return k;
-  const SeqRows m = seq_rows(a.r, k.seq);
-  k.len = a.c.lens[k.seq];
+  // uniform values, said to be: buffer descriptors are made from them
+  SeqRows m = seq_rows(a.r, k.seq);
+  m.first = __builtin_amdgcn_readfirstlane(m.first);
+  m.count = __builtin_amdgcn_readfirstlane(m.count);
+  k.len = __builtin_amdgcn_readfirstlane(a.c.lens[k.seq]);
   k.row0 = m.first;
   k.rows = m.count * a.gqa;
   const int last = (min(k.first + ROWS, k.rows) - 1) / a.gqa;      // row of the call
