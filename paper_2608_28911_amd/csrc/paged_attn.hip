@@ -77,7 +77,8 @@ __device__ inline void wave_order() {
 // What a workgroup works on: a tile of a sequence's rows, and a share of the
 // pages that it sees.
 struct Tile {
-  int seq, len, row0, rows, first;   // sequence, its tokens, its first row of the call, rows of (token, head), first of them
+  int seq, len, row0, count;         // sequence, its tokens, its first row of the call, and rows
+  int rows, first;                   // rows of (token, head), and the first of the tile's
   int pages, splits, split;          // pages the tile's last row sees, workgroups that share them, this one's place
   int part;                          // the tile's first partial and its counter
 };
@@ -89,35 +90,40 @@ struct Tile {
 // the sequences, 64 at a time.
 template <int ROWS, int NW>
 __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
-  struct Share { int tiles, pages; };
+  struct Share { int first, count, len, tiles, pages; };
   auto share = [&](int s) {
-    Share k = {0, 0};
+    Share k = {0, 0, 0, 0, 0};
     if (s < a.r.n_seqs) {
-      k.tiles = (seq_rows(a.r, s).count * a.gqa + ROWS - 1) / ROWS;
-      k.pages = (a.c.lens[s] + kPage - 1) / kPage;
+      const SeqRows m = seq_rows(a.r, s);
+      k.first = m.first;
+      k.count = m.count;
+      k.len = a.c.lens[s];
+      k.tiles = (m.count * a.gqa + ROWS - 1) / ROWS;
+      k.pages = (k.len + kPage - 1) / kPage;
     }
     return k;
   };
   Share mine = share(lane);
-  int64_t work = 0;
-  for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
-    const Share k = s0 ? share(s0 + lane) : mine;
+  int64_t work = int64_t(mine.tiles) * mine.pages;
+  for (int s0 = 64; s0 < a.r.n_seqs; s0 += 64) {
+    const Share k = share(s0 + lane);
     work += int64_t(k.tiles) * k.pages;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
-  const int64_t even = (work + a.target - 1) / a.target;
-  const int chunk = __builtin_amdgcn_readfirstlane(int(min(max(even, int64_t(NW)), int64_t(1) << 30)));
+  const int width = min(a.r.n_seqs, 64);           // lanes that hold a sequence
+  for (int d = 1; d < width; d <<= 1) work += __shfl_xor(work, d);
+  const uint32_t wl = __builtin_amdgcn_readfirstlane(int(work)), wh = __builtin_amdgcn_readfirstlane(int(work >> 32));
+  // past 2^31 pages (never few tiles): one workgroup a tile
+  const int even = wh || wl >> 31 ? INT32_MAX / 2 : int((wl + uint32_t(a.target) - 1u) / uint32_t(a.target));
+  const int chunk = max(even, NW);
   Tile k;
   k.seq = -1;
   int before = 0, parts = 0;
   for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
     if (s0) mine = share(s0 + lane);
-    const int splits = mine.pages > chunk ? (mine.pages + chunk - 1) / chunk : 1;
+    const int splits = mine.pages > chunk ? int(uint32_t(mine.pages + chunk - 1) / uint32_t(chunk)) : 1;
     const int n = mine.tiles * splits, held = splits > 1 ? n : 0;
     int incl = n, pincl = held;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < width; d <<= 1) {
       const int up = __shfl_up(incl, d), pup = __shfl_up(pincl, d);
       if (lane >= d) {
         incl += up;
@@ -128,28 +134,25 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
     if (above) {
       const int l = __ffsll((unsigned long long)above) - 1;
       const int at = flat - before - __builtin_amdgcn_readlane(incl - n, l), sp = __builtin_amdgcn_readlane(splits, l);
-      const int t = at / sp, tiles = __builtin_amdgcn_readlane(mine.tiles, l);
+      const int t = int(uint32_t(at) / uint32_t(sp)), tiles = __builtin_amdgcn_readlane(mine.tiles, l);
       k.seq = s0 + l;
       k.split = at - t * sp;
       k.part = parts + __builtin_amdgcn_readlane(pincl - held, l) + t * sp;
       k.first = (tiles - 1 - t) * ROWS;            // the last rows, which see the most, first
+      k.row0 = __builtin_amdgcn_readlane(mine.first, l);
+      k.count = __builtin_amdgcn_readlane(mine.count, l);
+      k.len = __builtin_amdgcn_readlane(mine.len, l);
       break;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
     parts += __builtin_amdgcn_readlane(pincl, 63);
   }
   if (k.seq < 0) return k;
-  // uniform values, said to be: buffer descriptors are made from them
-  SeqRows m = seq_rows(a.r, k.seq);
-  m.first = __builtin_amdgcn_readfirstlane(m.first);
-  m.count = __builtin_amdgcn_readfirstlane(m.count);
-  k.len = __builtin_amdgcn_readfirstlane(a.c.lens[k.seq]);
-  k.row0 = m.first;
-  k.rows = m.count * a.gqa;
-  const int last = (min(k.first + ROWS, k.rows) - 1) / a.gqa;      // row of the call
-  const int seen = k.len - m.count + last + 1;
+  k.rows = k.count * a.gqa;
+  const int last = int(uint32_t(min(k.first + ROWS, k.rows) - 1) / uint32_t(a.gqa));      // row of the call
+  const int seen = k.len - k.count + last + 1;
   k.pages = seen > 0 ? (seen + kPage - 1) / kPage : 0;
-  k.splits = max(1, (k.pages + chunk - 1) / chunk);
+  k.splits = max(1, int(uint32_t(k.pages + chunk - 1) / uint32_t(chunk)));
   return k;
 }
 
@@ -190,23 +193,61 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
   const int split = tl.split;
   if (tl.seq < 0 || split >= tl.splits) return;
 
+  // the rows' queries, and behind them the wave's first record: in flight together
+  int seen[NR];                                    // last token the row sees
+  uint4 qw[NR][NK];
+  const int m0 = tl.len - tl.count;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int row = tl.first + 16 * r + n < tl.rows ? tl.first + 16 * r + n : tl.first;
+    const int i = int(uint32_t(row) / uint32_t(a.gqa)), g = row - i * a.gqa;
+    seen[r] = m0 + i;
+    const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.sT + int64_t(head * a.gqa + g) * a.sH + 8 * kg;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) qw[r][k] = *reinterpret_cast<const uint4*>(src + 32 * k);
+  }
+  // the tile's first row sees the least: pages up to here need no mask
+  const int all_see = m0 + tl.first / a.gqa;
+  const int each = int(uint32_t(tl.pages + tl.splits - 1) / uint32_t(tl.splits));
+  const int p0 = split * each, p1 = min(p0 + each, tl.pages);
+  const int32_t* table = c.table + int64_t(tl.seq) * c.seq_pages;
+  // A wave's next record is loaded piece by piece as soon as the current one's
+  // piece has been used; past its last page, and for a page that is missing,
+  // the descriptor's size is 0 and the loads return zeros.
+  auto page_at = [&](int p) { return p < p1 ? __builtin_amdgcn_readfirstlane(table[p]) : -1; };
+  auto record = [&](int page) {
+    return __builtin_amdgcn_make_buffer_rsrc(paged_record_at(c, max(page, 0), a.layer, head), 0,
+                                             page < 0 ? 0 : paged_record(D, G), kBufferWord3);
+  };
+  auto load = [&](const __amdgpu_buffer_rsrc_t& rs, int offset) {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + offset, 0, 0));
+  };
+  // Metadata goes through LDS, a region for each wave: 16 lanes share a token's
+  __shared__ __align__(16) uint4 sm_meta[NW][32 * NG];
+  constexpr int MV = (32 * NG + 63) / 64;          // 16-byte loads of it
+  uint4 kw[NP], vw[NP], mw[MV];
+  int page = page_at(p0 + wave), next = page_at(p0 + wave + NW);
+  {
+    const auto rs = record(page);
+#pragma unroll
+    for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
+  }
+
   // the rows' queries as fp16 operands, each row scaled by a power of two so
   // that its largest value lies in [2^14, 2^15); slots 2, 3, 6, 7 carry 1/16
   half8v qf[NR][NK];
   float qs[NR][NG], cf[NR];
-  int seen[NR];                                    // last token the row sees
-  const int m0 = tl.len - tl.rows / a.gqa;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const int row = tl.first + 16 * r + n;
-    const bool valid = row < tl.rows;
-    const int i = (valid ? row : tl.first) / a.gqa, g = (valid ? row : tl.first) - i * a.gqa;
-    seen[r] = m0 + i;
-    const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.sT + int64_t(head * a.gqa + g) * a.sH + 8 * kg;
+    const bool valid = tl.first + 16 * r + n < tl.rows;
     uint32_t d[4 * NK];
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      const uint4 v = *reinterpret_cast<const uint4*>(src + 32 * k);
+      const uint4 v = qw[r][k];
       d[4 * k] = valid ? v.x : 0u;
       d[4 * k + 1] = valid ? v.y : 0u;
       d[4 * k + 2] = valid ? v.z : 0u;
@@ -253,35 +294,6 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
     for (int ct = 0; ct < NC; ++ct) o[r][ct] = float4v{0, 0, 0, 0};
   }
 
-  // the tile's first row sees the least: pages up to here need no mask
-  const int all_see = m0 + tl.first / a.gqa;
-  const int p0 = int(int64_t(tl.pages) * split / tl.splits), p1 = int(int64_t(tl.pages) * (split + 1) / tl.splits);
-  const int32_t* table = c.table + int64_t(tl.seq) * c.seq_pages;
-  // A wave's next record is loaded piece by piece as soon as the current one's
-  // piece has been used; past its last page, and for a page that is missing,
-  // the descriptor's size is 0 and the loads return zeros.
-  auto page_at = [&](int p) { return p < p1 ? __builtin_amdgcn_readfirstlane(table[p]) : -1; };
-  auto record = [&](int page) {
-    return __builtin_amdgcn_make_buffer_rsrc(paged_record_at(c, max(page, 0), a.layer, head), 0,
-                                             page < 0 ? 0 : paged_record(D, G), kBufferWord3);
-  };
-  auto load = [&](const __amdgpu_buffer_rsrc_t& rs, int offset) {
-    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + offset, 0, 0));
-  };
-  // Metadata goes through LDS, a region for each wave: 16 lanes share a token's
-  __shared__ __align__(16) uint4 sm_meta[NW][32 * NG];
-  constexpr int MV = (32 * NG + 63) / 64;          // 16-byte loads of it
-  uint4 kw[NP], vw[NP], mw[MV];
-  int page = page_at(p0 + wave), next = page_at(p0 + wave + NW);
-  {
-    const auto rs = record(page);
-#pragma unroll
-    for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
-#pragma unroll
-    for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
-  }
   for (int p = p0 + wave; p < p1; p += NW) {
     const auto rs = record(next);
     const int have = page < 0 ? 0 : tl.len;        // tokens of a missing page are past the end
