@@ -8,13 +8,16 @@
 //   scores  C[16 tokens][16 rows] = codes . q,   x = s_t (c.q) + z_t (sum q)
 //   values  C[16 channels][16 rows] = codes . w, w = p_t s_t, and the zeros'
 //           share sum_t p_t z_t is kept apart in fp32
-// A code enters as the fp16 subnormal c 2^-24 (bits 0..3 of a half) or
-// c 2^-20 (bits 4..7): one AND (and a shift for two of four) makes a pair, and
-// the other operand carries the 1/16 of the second kind.  A lane's 16-byte
-// loads of a record are its operands as they are, and the scores' layout
-// (lane: row lane mod 16, tokens 4 (lane div 16) + i) is the values' operand
-// layout, since the words of V hold their tokens in that order: the weights go
-// from one product to the next in registers.
+// A code enters as the half with its bits at 3..6 (c 2^-21, a subnormal) or
+// 7..10 (c 2^-17): a shift for two words of two and an AND each, and the other
+// operand carries the 1/16 of the second kind.  (The matrix unit aligns its
+// products by the operands' exponents as written: the lower a subnormal's
+// bits, the fewer of its product are kept.  With the codes at bits 0..3 and
+// 4..7, one shift less, the error of a score was some 20 times this.)  A lane's
+// 16-byte loads of a record are its operands but for that, and the scores'
+// layout (lane: row lane mod 16, tokens 4 (lane div 16) + i) is the values'
+// operand layout, since the words of V hold their tokens in that order: the
+// weights go from one product to the next in registers.
 //
 // Softmax: one pass with a running reference M per row.  It includes the
 // exponent of the largest V scale seen, so that w = 2^(x - M + 10) s_t lies
@@ -38,6 +41,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 // a tile is split, ceil(pages / chunk) is below twice pages / chunk: at most 2
 // kSlots partials, of which each tile's first also names its counter of
 // finished splits, each on a 256-byte line at the workspace's head.
+constexpr int kLeast = 4, kWhole = 8, kMostSplits = 64;
 constexpr int kSlots = 512, kCounterStride = 64, kCounterWords = 2 * kSlots * kCounterStride;
 constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx9 family)
 // fp16 weights: 2^10 at the reference, which may lag a record by 2^5 (below
@@ -45,24 +49,46 @@ constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx
 // bits down to 2^-20 of the largest
 constexpr float kHead = 10.0f, kLag = 5.0f;
 
-// 8 codes of a word as fp16: slots 0, 1, 4, 5 as c 2^-24, slots 2, 3, 6, 7 as c 2^-20
+// 8 codes of a word as fp16: slots 0, 1, 4, 5 as c 2^-21, slots 2, 3, 6, 7 as c 2^-17
+constexpr float kCode = 0x1p21f;
 __device__ inline half8v codes8(uint32_t w) {
-  const uint32_t h = w >> 8;
-  const uint4 v = make_uint4(w & 0x000F000Fu, w & 0x00F000F0u, h & 0x000F000Fu, h & 0x00F000F0u);
+  const uint32_t l = w << 3, h = w >> 5;
+  const uint4 v = make_uint4(l & 0x00780078u, l & 0x07800780u, h & 0x00780078u, h & 0x07800780u);
   return __builtin_bit_cast(half8v, v);
+}
+// codes of 128, as normal numbers: for the sums of the other operand
+constexpr float kSum = 0x1p14f;
+__device__ inline half8v sums8(bool some) {
+  const uint32_t l = some ? 0x04000400u : 0u, h = some ? 0x14001400u : 0u;
+  return __builtin_bit_cast(half8v, make_uint4(l, h, l, h));
 }
 
 __device__ inline float lo16(uint32_t m) { return float(__builtin_bit_cast(half2v, m)[0]); }
 __device__ inline float hi16(uint32_t m) { return float(__builtin_bit_cast(half2v, m)[1]); }
 
-// over the four lanes of a row (16 apart)
-__device__ inline float row_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+// Over the four lanes of a row (16 apart): rows of 16 lanes are exchanged in
+// registers, so that lane groups 0 and 1, 2 and 3, then both pairs meet.
+template <class F>
+__device__ inline float over_row(float x, F f) {
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t y = __float_as_uint(f(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const auto q = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
-__device__ inline float row_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+__device__ inline float row_max(float x) { return over_row(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ inline float row_sum(float x) { return over_row(x, [](float a, float b) { return a + b; }); }
+
+// the largest of the wave's values: within 16 lanes by DPP moves, then as above
+__device__ inline uint32_t wave_max(uint32_t x) {
+  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0xB1, 0xF, 0xF, true)));    // lane xor 1
+  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x4E, 0xF, 0xF, true)));    // lane xor 2
+  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x141, 0xF, 0xF, true)));   // mirror of 8 lanes
+  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x140, 0xF, 0xF, true)));   // mirror of 16
+  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max(uint32_t(p[0]), uint32_t(p[1]));
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(uint32_t(q[0]), uint32_t(q[1]));
 }
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -83,12 +109,22 @@ struct Tile {
   int part;                          // the tile's first partial and its counter
 };
 
-// The pages of a call are shared out by what the sequences really hold: each
-// workgroup takes `chunk` pages at most, the call's tiles times pages over the
-// workgroups wanted for a kv head (a.target), and a page for each wave at
-// least.  A workgroup finds its tile from its flat index by a prefix sum over
-// the sequences, 64 at a time.
-template <int ROWS, int NW>
+// The pages of a call are shared out by what the sequences really hold: the
+// call's tiles times pages over the workgroups wanted for a kv head (a.target)
+// make a share (`chunk`), which grows until as many workgroups do: one more
+// than fit the chip at once costs as much as a whole round (4 x 32k tokens, 8
+// waves a workgroup: 27 us instead of 41).  A sequence is split where it holds
+// more than a share and kWhole pages, into kMostSplits at most: joining costs
+// 2 us (500 tokens 7.0 us whole, 8.8 in two) and 0.05 more for each split.
+__device__ inline int splits_of(int pages, int chunk) {
+  if (pages <= max(chunk, kWhole)) return 1;
+  const int share = max(chunk, (pages + kMostSplits - 1) / kMostSplits);
+  return int(uint32_t(pages + share - 1) / uint32_t(share));
+}
+
+// A workgroup finds its tile from its flat index by a prefix sum over the
+// sequences, 64 at a time.
+template <int ROWS>
 __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
   struct Share { int first, count, len, tiles, pages; };
   auto share = [&](int s) {
@@ -114,13 +150,26 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
   const uint32_t wl = __builtin_amdgcn_readfirstlane(int(work)), wh = __builtin_amdgcn_readfirstlane(int(work >> 32));
   // past 2^31 pages (never few tiles): one workgroup a tile
   const int even = wh || wl >> 31 ? INT32_MAX / 2 : int((wl + uint32_t(a.target) - 1u) / uint32_t(a.target));
-  const int chunk = max(even, NW);
+  int chunk = max(even, kLeast);
+  if (a.r.n_seqs > 1 && a.r.n_seqs <= 64) {
+    int tiles = mine.tiles;
+    for (int d = 1; d < width; d <<= 1) tiles += __shfl_xor(tiles, d);
+    const int limit = max(a.target, 2 * __builtin_amdgcn_readfirstlane(tiles));
+#pragma unroll 1
+    for (int tries = 0; tries < 3; ++tries) {
+      int made = mine.tiles * splits_of(mine.pages, chunk);
+      for (int d = 1; d < width; d <<= 1) made += __shfl_xor(made, d);
+      made = __builtin_amdgcn_readfirstlane(made);
+      if (made <= limit) break;
+      chunk = int(float(chunk) * float(made) / float(limit)) + 1;
+    }
+  }
   Tile k;
   k.seq = -1;
-  int before = 0, parts = 0;
+  int before = 0, parts = 0, sp = 1;
   for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
     if (s0) mine = share(s0 + lane);
-    const int splits = mine.pages > chunk ? int(uint32_t(mine.pages + chunk - 1) / uint32_t(chunk)) : 1;
+    const int splits = splits_of(mine.pages, chunk);
     const int n = mine.tiles * splits, held = splits > 1 ? n : 0;
     int incl = n, pincl = held;
     for (int d = 1; d < width; d <<= 1) {
@@ -133,7 +182,8 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
     const uint64_t above = __ballot(before + incl > flat);
     if (above) {
       const int l = __ffsll((unsigned long long)above) - 1;
-      const int at = flat - before - __builtin_amdgcn_readlane(incl - n, l), sp = __builtin_amdgcn_readlane(splits, l);
+      const int at = flat - before - __builtin_amdgcn_readlane(incl - n, l);
+      sp = __builtin_amdgcn_readlane(splits, l);
       const int t = int(uint32_t(at) / uint32_t(sp)), tiles = __builtin_amdgcn_readlane(mine.tiles, l);
       k.seq = s0 + l;
       k.split = at - t * sp;
@@ -152,7 +202,7 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
   const int last = int(uint32_t(min(k.first + ROWS, k.rows) - 1) / uint32_t(a.gqa));      // row of the call
   const int seen = k.len - k.count + last + 1;
   k.pages = seen > 0 ? (seen + kPage - 1) / kPage : 0;
-  k.splits = max(1, int(uint32_t(k.pages + chunk - 1) / uint32_t(chunk)));
+  k.splits = min(splits_of(k.pages, chunk), sp);
   return k;
 }
 
@@ -183,25 +233,23 @@ template <int D>
 constexpr int partial_floats(int rows) { return rows * (D + 4); }
 
 template <int D, int G, int NR, int NW>
-__global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int NK = D / 32, NC = D / 16, NG = D / G, KG = G / 32, CG = G / 16, ROWS = 16 * NR;
   constexpr int CB = paged_code_bytes(D), NP = D / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const PagedView& c = a.c;
   const int head = blockIdx.x % c.n_kv_heads;
-  const Tile tl = tile_of<ROWS, NW>(a, blockIdx.x / c.n_kv_heads, lane);
+  const Tile tl = tile_of<ROWS>(a, blockIdx.x / c.n_kv_heads, lane);
   const int split = tl.split;
   if (tl.seq < 0 || split >= tl.splits) return;
 
   // the rows' queries, and behind them the wave's first record: in flight together
-  int seen[NR];                                    // last token the row sees
   uint4 qw[NR][NK];
   const int m0 = tl.len - tl.count;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int row = tl.first + 16 * r + n < tl.rows ? tl.first + 16 * r + n : tl.first;
     const int i = int(uint32_t(row) / uint32_t(a.gqa)), g = row - i * a.gqa;
-    seen[r] = m0 + i;
     const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.sT + int64_t(head * a.gqa + g) * a.sH + 8 * kg;
 #pragma unroll
     for (int k = 0; k < NK; ++k) qw[r][k] = *reinterpret_cast<const uint4*>(src + 32 * k);
@@ -267,22 +315,23 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
       for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[k][e]));
     mx = row_max(mx);
     const int ex = mx > 0.0f ? min(max(15 - __builtin_amdgcn_frexp_expf(mx), -100), 126) : 0;
-    cf[r] = __builtin_ldexpf(a.scale_log2e, 24 - ex);
-#pragma unroll
-    for (int j = 0; j < NG; ++j) qs[r][j] = 0.0f;
+    const float up = __builtin_ldexpf(1.0f, ex), up4 = __builtin_ldexpf(1.0f, ex - 4);
+    cf[r] = fmaxf(__builtin_ldexpf(a.scale_log2e * kCode, -ex), 0x1p-126f);
 #pragma unroll
     for (int k = 0; k < NK; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const _Float16 h = _Float16(__builtin_ldexpf(x[k][e], ex - (e & 2 ? 4 : 0)));
-        qf[r][k][e] = h;
-        qs[r][k / KG] += float(h) * (e & 2 ? 0x1p-20f : 0x1p-24f);
-      }
+      for (int e = 0; e < 8; ++e) qf[r][k][e] = _Float16(x[k][e] * (e & 2 ? up4 : up));
+    // sum q of each group, in the scores' units
 #pragma unroll
-    for (int j = 0; j < NG; ++j) qs[r][j] = row_sum(qs[r][j]);
+    for (int j = 0; j < NG; ++j) {
+      float4v acc = float4v{0, 0, 0, 0};
+#pragma unroll
+      for (int k = j * KG; k < (j + 1) * KG; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(sums8(true), qf[r][k], acc, 0, 0, 0);
+      qs[r][j] = acc[0] * (kSum / kCode);
+    }
   }
 
-  float4v o[NR][NC];
+  float4v o[NR][NC], ws[NR];                       // ws: lane group kg holds group kg's (one group: every lane)
   float M[NR], l[NR], az[NR][NG];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
@@ -290,6 +339,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
     l[r] = 0.0f;
 #pragma unroll
     for (int j = 0; j < NG; ++j) az[r][j] = 0.0f;
+    ws[r] = float4v{0, 0, 0, 0};
 #pragma unroll
     for (int ct = 0; ct < NC; ++ct) o[r][ct] = float4v{0, 0, 0, 0};
   }
@@ -354,21 +404,20 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
     const int t0 = p * kPage + 4 * kg;             // the lane's first token
     if (p * kPage + kPage - 1 > all_see || have == 0) {   // not every row sees every token
 #pragma unroll
-      for (int r = 0; r < NR; ++r)
+      for (int r = 0; r < NR; ++r) {
+        // the last token the row sees; worked out here, not kept in a register
+        int row = tl.first + 16 * r + n;
+        __asm__ volatile("" : "+v"(row));
+        const int seen = m0 + int(uint32_t(min(row, tl.rows - 1)) / uint32_t(a.gqa));
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[r][tt][e] = t0 + 16 * tt + e > min(seen[r], have - 1) ? -INFINITY : x[r][tt][e] * cf[r];
-    } else {
-#pragma unroll
-      for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) x[r][tt] *= cf[r];
+          for (int e = 0; e < 4; ++e) x[r][tt][e] = t0 + 16 * tt + e > min(seen, have - 1) ? -INFINITY : x[r][tt][e];
+      }
     }
 
     // the reference: row maximum plus the exponent of the record's largest V scale
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) smax = max(smax, uint32_t(__shfl_xor(int(smax), d)));
+    smax = wave_max(smax);
     const float se = float(int(smax >> 10)) - 14.0f;
     float ref[NR];
     bool move = false;
@@ -380,7 +429,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
       for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[r][tt][e]);
-      cand[r] = row_max(mx) + se;
+      cand[r] = fmaf(row_max(mx), cf[r], se);
       move |= cand[r] > M[r] + kLag;
     }
     if (__any(move)) {
@@ -392,6 +441,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
         l[r] *= f;
 #pragma unroll
         for (int j = 0; j < NG; ++j) az[r][j] *= f;
+        ws[r] *= f;
 #pragma unroll
         for (int ct = 0; ct < NC; ++ct) o[r][ct] *= f;
       }
@@ -405,7 +455,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
       for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[r][tt][e] = exp2_fast(x[r][tt][e] - ref[r]);
+          x[r][tt][e] = exp2_fast(fmaf(x[r][tt][e], cf[r], -ref[r]));
           l[r] += x[r][tt][e];
         }
     const uint32_t* vd = reinterpret_cast<const uint32_t*>(vw);
@@ -424,11 +474,18 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
           for (int r = 0; r < NR; ++r) {
             const _Float16 w = _Float16(x[r][tt][e] * ss);
             wf[r][tt >> 1][4 * (tt & 1) + e] = w;
-            az[r][j] = fmaf(float(w), e & 2 ? -120.0f : -7.5f, fmaf(x[r][tt][e], mid, az[r][j]));
+            az[r][j] = fmaf(x[r][tt][e], mid, az[r][j]);
           }
         }
       }
       if (NG > 1) __builtin_amdgcn_sched_barrier(0);
+      // sums of the rounded weights (of several groups, each in its own four
+      // rows of the result)
+      const half8v ones = sums8(NG == 1 || n >> 2 == j);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) ws[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, wf[r][st], ws[r], 0, 0, 0);
       // values
 #pragma unroll
       for (int ct = j * CG; ct < (j + 1) * CG; ++ct)
@@ -446,6 +503,9 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
 
   // the waves' states merge in LDS, 16 rows at a time; then the tile's output,
   // or the split's partial
+  // (the lane's number made anew: kept over the loop it would be spilled)
+  const int lane2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)), tid = 64 * wave + lane2;
+  const int n2 = lane2 & 15, kg2 = lane2 >> 4;
   constexpr int PITCH = D + 4, LPR = D / 4, NT = 64 * NW;   // LPR: threads of an output row
   __shared__ float sm_m[NW][ROWS], sm_l[NW][ROWS];
   __shared__ __align__(16) float sm_o[NW][16][PITCH];
@@ -453,10 +513,14 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
   for (int r = 0; r < NR; ++r) {
     l[r] = row_sum(l[r]);
 #pragma unroll
-    for (int j = 0; j < NG; ++j) az[r][j] = row_sum(az[r][j]);
-    if (kg == 0) {
-      sm_m[wave][16 * r + n] = M[r];
-      sm_l[wave][16 * r + n] = l[r];
+    for (int j = 0; j < NG; ++j) {
+      // the zeros' share, less what the rounded weights give to 7.5
+      const float w = NG == 1 ? ws[r][0] : __shfl(ws[r][0], 16 * j + n2);
+      az[r][j] = fmaf(w, -7.5f * kSum, row_sum(az[r][j]));
+    }
+    if (kg2 == 0) {
+      sm_m[wave][16 * r + n2] = M[r];
+      sm_l[wave][16 * r + n2] = l[r];
     }
   }
   __syncthreads();
@@ -468,16 +532,16 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
     if (16 * r >= rows) break;
     float Mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) Mx = fmaxf(Mx, sm_m[w][16 * r + n]);
+    for (int w = 0; w < NW; ++w) Mx = fmaxf(Mx, sm_m[w][16 * r + n2]);
     // a row without a token keeps its NaN, if it has one, and zeros else
     const float f = M[r] == -INFINITY ? 1.0f : exp2_fast(M[r] - Mx);
-    if (16 * r + n < rows) {
+    if (16 * r + n2 < rows) {
 #pragma unroll
       for (int ct = 0; ct < NC; ++ct)
-        *reinterpret_cast<float4v*>(&sm_o[wave][n][16 * ct + 4 * kg]) = (o[r][ct] * 0x1p24f + az[r][ct / CG]) * f;
+        *reinterpret_cast<float4v*>(&sm_o[wave][n2][16 * ct + 4 * kg2]) = (o[r][ct] * kCode + az[r][ct / CG]) * f;
     }
     __syncthreads();
-    for (int at = threadIdx.x; at < min(rows - 16 * r, 16) * LPR; at += NT) {
+    for (int at = tid; at < min(rows - 16 * r, 16) * LPR; at += NT) {
       const int rr = at / LPR, ch = at % LPR * 4;
       float My = -INFINITY, L = 0.0f;
 #pragma unroll
@@ -511,7 +575,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
   __shared__ int sm_last;
   __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     uint32_t* counter = reinterpret_cast<uint32_t*>(a.ws) + unit * kCounterStride;
     const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sm_last = before + 1 == uint32_t(tl.splits);
@@ -522,7 +586,7 @@ __global__ __launch_bounds__(64 * NW, D / G * NR >= 4 && NR > 1 ? 1 : 2) void pa
   __asm__ volatile("" ::: "memory");
   // NT/LPR rows at once: where there are fewer, the rest share a row's splits
   const int lanes = rows >= NT / LPR ? 1 : NT / LPR / rows;       // threads to a (row, 4 channels)
-  const int at0 = threadIdx.x / LPR, ch = threadIdx.x % LPR * 4, part0 = at0 % lanes;
+  const int at0 = tid / LPR, ch = tid % LPR * 4, part0 = at0 % lanes;
   constexpr int kFar = 16;                                        // cache policy sc1, as agent-scope loads
   const auto far = __builtin_amdgcn_make_buffer_rsrc(parts, 0, tl.splits * partial_floats<D>(ROWS) * 4, kBufferWord3);
   float* sm_j = &sm_o[0][0][0];                                   // [row][lane of it][D + 4]
@@ -597,10 +661,9 @@ int launch(PagedAttnArgs a, hipStream_t s) {
   int64_t wanted = kSlots * 4 / NW / a.c.n_kv_heads;
   if (wanted < 1) wanted = 1;
   a.target = int(wanted);
-  // every tile, and a share of the wanted ones where pages are split; no more
-  // than a page a workgroup
+  // every tile, and a share of the wanted ones where pages are split
   int64_t grid = tiles + wanted;
-  if (a.c.seq_pages <= NW) grid = tiles;
+  if (a.c.seq_pages <= kWhole) grid = tiles;
   hipLaunchKernelGGL((paged_attn_kernel<D, G, NR, NW>), dim3(unsigned(grid * a.c.n_kv_heads)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
@@ -608,7 +671,14 @@ int launch(PagedAttnArgs a, hipStream_t s) {
 template <int D, int G>
 int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t rows = (a.r.n_rows * a.gqa + a.r.n_seqs - 1) / a.r.n_seqs;   // of a sequence, on average
-  if (rows <= 16) return launch<D, G, 1, 8>(a, s);
+  // A workgroup of 8 waves for a single sequence: half as many splits to join
+  // (one token over 32k tokens 14.9 us, with 4 waves 17.7); else of 4, two of
+  // which hide each other's beginnings and ends (8 x 4k tokens 14.1, 21.5)
+  if (rows <= 16 && a.r.n_seqs == 1) return launch<D, G, 1, 8>(a, s);
+  if (rows <= 16) return launch<D, G, 1, 4>(a, s);
+  // as above: 5 tokens of 4 x 32k, with 8 waves 35.5 us, with 4 42.6; 8 chunks
+  // of 64 tokens, which fill the chip, 65.5 and 56.7
+  if (rows * a.r.n_seqs * a.c.n_kv_heads <= 32 * 128) return launch<D, G, 2, 8>(a, s);
   return launch<D, G, 2, 4>(a, s);
 }
 
