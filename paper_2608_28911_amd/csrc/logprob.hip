@@ -11,6 +11,8 @@
 // which happens k ln(n/k) times for n logits in random order.
 #include <hip/hip_fp16.h>
 
+#include <type_traits>
+
 #include "paged.h"
 
 namespace semkv {
@@ -69,11 +71,29 @@ __device__ inline void raise(Sums& a, float m) {          // m >= a.m
   a.m = m;
 }
 
-__device__ inline Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m);
-  raise(a, m);
-  raise(b, m);
-  return {m, a.S + b.S, a.T + b.T};
+// Within 16 lanes by DPP moves, then rows of 16 lanes are exchanged in
+// registers; every lane has the result.
+template <class F>
+__device__ inline float over_wave(float x, F f) {
+  auto dpp = [](float v, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  x = f(x, dpp(x, std::integral_constant<int, 0xB1>{}));     // lane xor 1
+  x = f(x, dpp(x, std::integral_constant<int, 0x4E>{}));     // lane xor 2
+  x = f(x, dpp(x, std::integral_constant<int, 0x141>{}));    // mirror of 8 lanes
+  x = f(x, dpp(x, std::integral_constant<int, 0x140>{}));    // mirror of 16
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t y = __float_as_uint(f(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const auto q = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// The lanes' states joined, in every lane.
+__device__ inline Sums join_wave(Sums s) {
+  raise(s, over_wave(s.m, [](float a, float b) { return fmaxf(a, b); }));
+  auto add = [](float a, float b) { return a + b; };
+  return {s.m, over_wave(s.S, add), over_wave(s.T, add)};
 }
 
 // Order of logits as unsigned integers: NaN above everything, -0 as +0; 0 is
@@ -113,6 +133,10 @@ __device__ inline void keep_all(Kept& s, bool may, uint32_t h, uint32_t l, int k
   }
 }
 
+__device__ inline float logit_of(uint32_t order) {
+  return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
+
 // The k-th largest of the lanes' orders (its upper 24 bits): as many lanes hold
 // a logit that is no smaller, so a row's k likeliest are not below it.
 __device__ inline uint32_t kth_order(uint32_t h, int k) {
@@ -145,10 +169,6 @@ __device__ inline void finish(const TokenArgs& a, int64_t row, const Sums& s) {
     }
     a.logp[at] = a.negate && target != -1 ? -v : v;
   }
-}
-
-__device__ inline float logit_of(uint32_t order) {
-  return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
 __device__ inline void finish_top(const TokenArgs& a, int64_t row, const Sums& s, uint32_t h, uint32_t l, int i) {
@@ -226,14 +246,15 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
       if (__any(most > last)) {
         // while the list fills, the lanes' maxima bound what it can end with
         const uint32_t least = max(last, kth_order(most, k));
+        const float bound = least > order_of(-INFINITY) ? logit_of(least) : -INFINITY;   // the same order, as a logit
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int64_t at = v + lane + u * NT;
-          if (!__any(at < v1 && order_of(mx[u]) >= least)) continue;
+          if (!__any(at < v1 && mx[u] >= bound)) continue;
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const uint32_t h = order_of(e[u][i]);
-            keep_all(kept, at < v1 && h >= least, h, ~uint32_t(head + at * V + i), k, lane);
+            const bool may = at < v1 && e[u][i] >= bound;
+            if (__any(may)) keep_all(kept, may, order_of(e[u][i]), ~uint32_t(head + at * V + i), k, lane);
           }
         }
         last = __builtin_amdgcn_readlane(kept.hi, k - 1);
@@ -244,8 +265,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
   const int64_t tail = head + vecs * V;
   if (blockIdx.y + 1 == a.nsplit && wave == 0) single(tail + lane, tail + lane < a.vocab);
 
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) s = join(s, Sums{__shfl_xor(s.m, d), __shfl_xor(s.S, d), __shfl_xor(s.T, d)});
+  s = join_wave(s);
   if (lane == 0) sm[wave] = s;
   if (TOP && lane < k) {
     sm_hi[wave * k + lane] = kept.hi;
@@ -253,9 +273,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
   }
   __syncthreads();
   if (wave != 0) return;
-  s = sm[0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) s = join(s, sm[w]);
+  s = join_wave(lane < WAVES ? sm[lane] : Sums{kFloor, 0.0f, 0.0f});
   if constexpr (TOP) {
     for (int i = k; i < WAVES * k; i += 64) {              // the other waves' keys into wave 0's
       const bool valid = i + lane < WAVES * k;
@@ -289,10 +307,14 @@ __global__ __launch_bounds__(64) void token_merge_kernel(TokenArgs a) {
   Kept kept = {0u, 0u};
   for (int i = lane; i < a.nsplit; i += 64) {
     const uint32_t* q = p + i * partial_words(k);
-    s = join(s, Sums{__uint_as_float(q[0]), __uint_as_float(q[1]), __uint_as_float(q[2])});
+    Sums t = {__uint_as_float(q[0]), __uint_as_float(q[1]), __uint_as_float(q[2])};
+    const float m = fmaxf(s.m, t.m);
+    raise(s, m);
+    raise(t, m);
+    s.S += t.S;
+    s.T += t.T;
   }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) s = join(s, Sums{__shfl_xor(s.m, d), __shfl_xor(s.S, d), __shfl_xor(s.T, d)});
+  s = join_wave(s);
   if (lane == 0) finish(a, row, s);
   if (k == 0) return;
   for (int i = 0; i < a.nsplit * k; i += 64) {

@@ -3,6 +3,8 @@
 // compact).
 #include <hip/hip_fp16.h>
 
+#include <type_traits>
+
 #include "paged.h"
 
 namespace semkv {
@@ -185,22 +187,22 @@ __global__ __launch_bounds__(1024) void paged_reserve_kernel(PagedView c, const 
   if (mine) c.lens[t] = len + n;
 }
 
-// The copies of shared last pages: 16 KB a workgroup.
+// The copies of shared last pages: 16 KB a workgroup, every load in flight.
 constexpr int kCopyVecs = 1024;
 __global__ __launch_bounds__(256) void paged_copy_kernel(PagedView c) {
   const int s = blockIdx.y, src = c.cow[2 * s];
   if (src < 0) return;
-  const int64_t bytes = int64_t(c.record) * c.n_layers * c.n_kv_heads, vecs = bytes / 16;
+  const int64_t bytes = int64_t(c.record) * c.n_layers * c.n_kv_heads, last = bytes / 16 - 1;
   const uint4* from = reinterpret_cast<const uint4*>(c.pool + src * bytes);
   uint4* to = reinterpret_cast<uint4*>(c.pool + c.cow[2 * s + 1] * bytes);
   const int64_t i0 = int64_t(blockIdx.x) * kCopyVecs + threadIdx.x;
-  uint4 v[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (i0 + 256 * k < vecs) v[k] = from[i0 + 256 * k];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (i0 + 256 * k < vecs) to[i0 + 256 * k] = v[k];
+  const int64_t i1 = min(i0 + 256, last), i2 = min(i0 + 512, last), i3 = min(i0 + 768, last);   // the last may be copied again
+  if (i0 > last) return;
+  const uint4 v0 = from[i0], v1 = from[i1], v2 = from[i2], v3 = from[i3];
+  to[i0] = v0;
+  to[i1] = v1;
+  to[i2] = v2;
+  to[i3] = v3;
 }
 
 // fork, first half: the new rows, and a count more for each page that a
@@ -260,13 +262,17 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedView c, const int
   }
 }
 
-// compact, second step: one workgroup builds one record of a fresh page.  K: a
-// row is D/32 pieces' 16-byte lanes (D = 128; half lanes at D = 64), moved as
-// words.  V: a word holds 8 tokens of a channel; each nibble comes from its
-// own token's word.
+// compact, second step: one workgroup builds one record of a fresh page.  A
+// K row is 32 D/16 bytes in four places (lane groups), of 16 bytes at D = 128
+// and 8 at 64, each moved whole.  A V piece of 16 bytes holds two channels
+// (D/32 pieces of 64 lanes) of the 16 tokens whose (t div 4) mod 4 is its lane
+// group; a thread builds one of the destination from one load for each of its
+// tokens, neighbouring lanes of neighbouring channels.  Memory-bound: tokens
+// are in ascending order, so their loads meet the same lines in the L1.
 template <int D>
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedView c, const int32_t* keep, int64_t ld) {
   constexpr int KI = D / 32;                       // K words of a row and lane
+  constexpr int CB = paged_code_bytes(D);
   __shared__ const uint8_t* rec_of[kPage];         // record of each kept token, null: none
   __shared__ int slot_of[kPage];
   const int s = blockIdx.y, tid = threadIdx.x;
@@ -292,35 +298,32 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedView c, const int3
   }
   __syncthreads();
   uint8_t* out = paged_record_at(c, c.list[c.base[s] + blockIdx.x], layer, head);
-  constexpr int CB = paged_code_bytes(D);
-  uint32_t* ok = reinterpret_cast<uint32_t*>(out);
-  for (int i = tid; i < kPage * D / 8; i += 256) {      // word i of the destination: piece, lane, w
-    const int w = i & 3, lane = (i >> 2) & 63, x = 4 * (i >> 8) + w;
-    const int t = 16 * (x / KI) + (lane & 15), blk = x % KI;
+  {
+    using Row = typename std::conditional<D == 128, uint4, uint2>::type;
+    const int t = tid & 63, g = tid >> 6;          // token, lane group
     const uint8_t* rec = rec_of[t];
-    uint32_t v = 0;
-    if (rec) {
-      const int st = slot_of[t], sx = (st / 16) * KI + blk;
-      v = reinterpret_cast<const uint32_t*>(rec)[((sx >> 2) * 64 + (lane & 48) + (st & 15)) * 4 + (sx & 3)];
-    }
-    ok[i] = v;
+    const int st = slot_of[t];
+    // word tile * KI, lane 16 g + t mod 16: piece, lane, word
+    auto at = [&](int slot) { return (((slot / 16) * KI >> 2) * 64 + 16 * g + (slot & 15)) * 4 + ((slot / 16) * KI & 3); };
+    Row v = {};
+    if (rec) v = *reinterpret_cast<const Row*>(reinterpret_cast<const uint32_t*>(rec) + at(st));
+    *reinterpret_cast<Row*>(reinterpret_cast<uint32_t*>(out) + at(t)) = v;
   }
-  uint32_t* ov = reinterpret_cast<uint32_t*>(out + CB);
-  for (int i = tid; i < kPage * D / 8; i += 256) {
-    const int w = i & 3, lane = (i >> 2) & 63, x = 4 * (i >> 8) + w;
-    const int t0 = 32 * (x & 1) + 4 * (lane >> 4);
-    uint32_t v = 0;
+  for (int i = tid; i < 64 * KI; i += 256) {       // piece and lane of V
+    const int lane = i & 63, piece = i >> 6, t0 = 4 * (lane >> 4);
+    uint32_t w[4] = {0, 0, 0, 0};                  // channels 32 piece + m and + 16, tokens 0..31 and 32..63
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = t0 + 16 * (j >> 2) + (j & 3);
+    for (int k = 0; k < 16; ++k) {
+      const int t = t0 + 16 * (k >> 2) + (k & 3), j = ((k >> 2) & 1) * 4 + (k & 3), sh = 4 * (j >> 1) + 16 * (j & 1);
       const uint8_t* rec = rec_of[t];
-      if (!rec) continue;
-      const int st = slot_of[t], sx = (x & ~1) | (st >> 5), sj = ((st >> 4) & 1) * 4 + (st & 3);
-      const uint32_t word = reinterpret_cast<const uint32_t*>(rec + CB)[((sx >> 2) * 64 + ((st >> 2) & 3) * 16 + (lane & 15)) * 4 + (sx & 3)];
-      const uint32_t nib = (word >> (4 * (sj >> 1) + 16 * (sj & 1))) & 15u;
-      v |= nib << (4 * (j >> 1) + 16 * (j & 1));
+      const int st = slot_of[t], sj = ((st >> 4) & 1) * 4 + (st & 3), ssh = 4 * (sj >> 1) + 16 * (sj & 1);
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (rec) v = reinterpret_cast<const uint4*>(rec + CB)[piece * 64 + ((st >> 2) & 3) * 16 + (lane & 15)];
+      const uint32_t lo = st >> 5 ? v.y : v.x, hi = st >> 5 ? v.w : v.z;
+      w[k >> 3] |= ((lo >> ssh) & 15u) << sh;
+      w[2 + (k >> 3)] |= ((hi >> ssh) & 15u) << sh;
     }
-    ov[i] = v;
+    reinterpret_cast<uint4*>(out + CB)[i] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   // metadata: [K or V][group][token]
   uint32_t* om = reinterpret_cast<uint32_t*>(out + 2 * CB);
@@ -398,24 +401,31 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
   const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
   if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
-  if (*c.stalled) return;
+  const int stalled = *c.stalled;
   const PageWork w = page_work(c, a.r, blockIdx.x);
-  if (w.seq < 0) return;
-  if (w.page < 0 || c.refs[w.page] > 1) {
+  if (w.seq < 0 || stalled) return;
+  const int holders = c.refs[max(w.page, 0)];
+  const bool mine = slot >= w.lo && slot < w.hi;
+  // both rows are loaded before the page's holders are looked at
+  uint4 in[2][Q / 8];
+  const int64_t from = int64_t(blockIdx.z) * a.sL + (w.row0 + (mine ? slot : w.lo)) * a.sT + head * a.sH + q * Q;
+#pragma unroll
+  for (int i = 0; i < Q / 8; ++i) {
+    in[0][i] = reinterpret_cast<const uint4*>(a.K + from)[i];
+    in[1][i] = reinterpret_cast<const uint4*>(a.V + from)[i];
+  }
+  if (w.page < 0 || holders > 1) {
     if (tid == 0) atomicOr(c.status, kBad);
     return;
   }
-  const bool mine = slot >= w.lo && slot < w.hi;
   uint8_t* rec = paged_record_at(c, w.page, layer, head);
   bool bad = false;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    const uint16_t* X = kv ? a.V : a.K;
-    const uint16_t* src = X + int64_t(blockIdx.z) * a.sL + (w.row0 + (mine ? slot : w.lo)) * a.sT + head * a.sH + q * Q;
     float x[Q];
 #pragma unroll
     for (int i = 0; i < Q / 8; ++i) {
-      const uint4 v = reinterpret_cast<const uint4*>(src)[i];
+      const uint4 v = in[kv][i];
       const uint32_t d[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -498,7 +508,8 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
 }
 
 // One workgroup returns the rows of one (page, layer, kv head): the record
-// goes to LDS, four lanes take a token row.
+// goes to LDS, a row's values leave in 16-byte stores of neighbouring lanes.
+// Memory-bound.
 template <int DT>
 __device__ inline void store8(void* p, int64_t at, const float (&v)[8]) {
   if constexpr (DT == 2) {
@@ -542,12 +553,17 @@ __device__ inline void early_rows(const PagedReadArgs& a, int head) {
   }
 }
 
+// The record's words in LDS, with room between runs of 32 and of 256 words so
+// that the lanes of a row's neighbouring channels read from different banks.
+__device__ inline int spread(int word) { return word + (word >> 5) * 4 + (word >> 8) * 8; }
+
 template <int D, int DT>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
-  constexpr int Q = D / 4, CB = paged_code_bytes(D), KI = D / 32;
-  __shared__ __align__(16) uint32_t rec[paged_record(D, 32) / 4];
+  constexpr int CB = paged_code_bytes(D), KI = D / 32, LPR = D / 8;   // LPR: threads of a row, 8 channels each
+  constexpr int WORDS = paged_record(D, 32) / 4;
+  __shared__ __align__(16) uint32_t rec[WORDS + WORDS / 32 * 4 + WORDS / 256 * 8];
   const PagedView& c = a.c;
-  const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
+  const int tid = threadIdx.x;
   const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
   if (blockIdx.x == 0) {
     if (blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
@@ -555,37 +571,33 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
   }
   const PageWork w = page_work(c, a.r, blockIdx.x);
   if (w.seq < 0) return;
-  if (w.page >= 0) {
-    const uint4* src = reinterpret_cast<const uint4*>(paged_record_at(c, w.page, layer, head));
-    for (int i = tid; i < c.record / 16; i += 256) reinterpret_cast<uint4*>(rec)[i] = src[i];
-  }
+  const uint4* src = reinterpret_cast<const uint4*>(paged_record_at(c, max(w.page, 0), layer, head));
+  for (int i = tid; i < c.record / 16; i += 256)
+    *reinterpret_cast<uint4*>(rec + spread(4 * i)) = w.page >= 0 ? src[i] : make_uint4(0, 0, 0, 0);
   __syncthreads();
-  if (slot < w.lo || slot >= w.hi) return;
-  const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + w.row0 + slot) * c.n_kv_heads + head) * D + q * Q;
-  const int groups = D / c.group;
+  const int groups = D / c.group, ch = tid % LPR * 8;
+  for (int slot = tid / LPR; slot < kPage; slot += 256 / LPR) {
+    if (slot < w.lo || slot >= w.hi) continue;
+    const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + w.row0 + slot) * c.n_kv_heads + head) * D + ch;
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    const uint32_t* words = rec + kv * CB / 4;
-    const uint32_t* meta = rec + 2 * CB / 4 + kv * groups * kPage;
-#pragma unroll
-    for (int i = 0; i < Q; i += 8) {
-      const int ch = q * Q + i;
-      const uint32_t m = w.page >= 0 ? meta[ch / c.group * kPage + slot] : 0u;
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint32_t m = rec[spread(2 * CB / 4 + (kv * groups + ch / c.group) * kPage + slot)];
       const float sc = h2f(m & 0xFFFFu), z = h2f(m >> 16);
       float v[8];
       if (kv == 0) {
         const int x = (slot / 16) * KI + ch / 32;
-        const uint32_t word = w.page >= 0 ? words[((x >> 2) * 64 + ((ch & 31) >> 3) * 16 + (slot & 15)) * 4 + (x & 3)] : 0u;
+        const uint32_t word = rec[spread(((x >> 2) * 64 + ((ch & 31) >> 3) * 16 + (slot & 15)) * 4 + (x & 3))];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = fmaf(float((word >> (4 * (j >> 1) + 16 * (j & 1))) & 15u), sc, z);
       } else {
         const int x = (ch / 16) * 2 + slot / 32, j = ((slot >> 4) & 1) * 4 + (slot & 3);
         const int sh = 4 * (j >> 1) + 16 * (j & 1);
-        const uint32_t* p = words + ((x >> 2) * 64 + ((slot >> 2) & 3) * 16 + (ch & 15)) * 4 + (x & 3);
+        // 8 channels: within 32 words
+        const uint32_t* p = rec + spread(CB / 4 + ((x >> 2) * 64 + ((slot >> 2) & 3) * 16 + (ch & 15)) * 4 + (x & 3));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(float(w.page >= 0 ? (p[4 * e] >> sh) & 15u : 0u), sc, z);
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(float((p[4 * e] >> sh) & 15u), sc, z);
       }
-      store8<DT>(kv ? a.V : a.K, at + i, v);
+      store8<DT>(kv ? a.V : a.K, at, v);
     }
   }
 }
