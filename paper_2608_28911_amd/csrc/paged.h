@@ -51,7 +51,7 @@ struct PagedWriteArgs {
   PagedRows r;
   const uint16_t* K; const uint16_t* V;
   int64_t sL, sT, sH;
-  int32_t layer0, layers, bf16;
+  int32_t layer0, layers, bf16, parts;
 };
 
 struct PagedReadArgs {
@@ -123,7 +123,7 @@ int launch_paged_assign(const PagedView& c, const int32_t* lens, const int32_t* 
 int launch_paged_reserve(const PagedView& c, const int32_t* n_new, hipStream_t s);
 int launch_paged_fork(const PagedView& c, const int32_t* parent, hipStream_t s);
 int launch_paged_compact(const PagedView& c, const int32_t* keep, int64_t ld, const int32_t* n_keep, hipStream_t s);
-int launch_paged_write(const PagedWriteArgs& a, hipStream_t s);
+int launch_paged_write(PagedWriteArgs a, hipStream_t s);
 int launch_paged_read(const PagedReadArgs& a, hipStream_t s);
 size_t paged_attn_workspace(int d);
 int launch_paged_attn(PagedAttnArgs a, size_t ws_bytes, hipStream_t s);

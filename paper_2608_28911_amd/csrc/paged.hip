@@ -384,120 +384,219 @@ __device__ inline void check_rows(const PagedView& c, const PagedRows& r) {
   }
 }
 
-// One workgroup quantizes the rows of one (page, layer, kv head).  Four lanes
-// own a token row, D/4 channels each, for K and then for V; the codes go to
-// LDS as bytes and come out as the words of the record's layout.  A page that
-// the rows fill only in part keeps its other rows: K words belong to one row,
-// V words hold 8 tokens and are merged with what is there.
+// Group parameters as fp16, saturated, and a code against the stored pair.
+struct Affine {
+  uint32_t bits;               // scale | zero << 16
+  float zero, inv;
+  __device__ Affine(float mn, float mx) {
+    const uint32_t zb = f2h(fminf(fmaxf(mn, -65504.0f), 65504.0f) + 0.0f);
+    zero = h2f(zb);
+    const uint32_t sb = f2h(fminf(fmaxf((mx - zero) / 15.0f, 0.0f), 65504.0f));
+    const float scale = h2f(sb);
+    inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+    bits = sb | zb << 16;
+  }
+  __device__ uint32_t code(float x) const {
+    return uint32_t(fminf(fmaxf(__builtin_rintf((x - zero) * inv), 0.0f), 15.0f));
+  }
+};
+
+__device__ inline bool finite(float x) { return fabsf(x) < INFINITY; }     // false for NaN
+
+template <int BF>
+__device__ inline void unpack2(uint32_t d, float& a, float& b) {
+  if constexpr (BF) {
+    a = __uint_as_float(d << 16);
+    b = __uint_as_float(d & 0xFFFF0000u);
+  } else {
+    a = h2f(d & 0xFFFFu);
+    b = h2f(d >> 16);
+  }
+}
+
+// f over runs of N = 2, 4, 8, 16, 32 or 64 lanes, in all of them: DPP moves
+// within 16 lanes, rows of 16 exchanged in registers beyond.
+template <int N, class F>
+__device__ inline float over_lanes(float x, F f) {
+  auto dpp = [](float v, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  x = f(x, dpp(x, std::integral_constant<int, 0xB1>{}));                   // lane xor 1
+  if constexpr (N >= 4) x = f(x, dpp(x, std::integral_constant<int, 0x4E>{}));     // lane xor 2
+  if constexpr (N >= 8) x = f(x, dpp(x, std::integral_constant<int, 0x141>{}));    // mirror of 8 lanes
+  if constexpr (N >= 16) x = f(x, dpp(x, std::integral_constant<int, 0x140>{}));   // mirror of 16
+  if constexpr (N >= 32) {
+    const uint32_t u = __float_as_uint(x);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  if constexpr (N >= 64) {
+    const uint32_t u = __float_as_uint(x);
+    const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  }
+  return x;
+}
+template <int N>
+__device__ inline float min_over(float x) { return over_lanes<N>(x, [](float a, float b) { return fminf(a, b); }); }
+template <int N>
+__device__ inline float max_over(float x) { return over_lanes<N>(x, [](float a, float b) { return fmaxf(a, b); }); }
+
+// Whether every lane of this lane's run of N says so.
+template <int N>
+__device__ inline bool all_of(bool ok) {
+  const uint64_t bad = __ballot(!ok);
+  if constexpr (N == 64) return bad == 0;
+  else return (bad >> (threadIdx.x & 63 & ~(N - 1)) & ((uint64_t(1) << N) - 1)) == 0;
+}
+
+// A page's only row of the call (a generated token): one wave, two channels a
+// lane.  A K word is four lanes'; a V word is one channel of 8 tokens, of which
+// the row's nibble is replaced.
+template <int D, int G, int BF>
+__device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uint8_t* rec, int z, int kv, int holders) {
+  constexpr int CB = paged_code_bytes(D), KI = D / 32;
+  const int lane = threadIdx.x & 63, head = blockIdx.y, slot = w.lo;
+  const bool on = lane < D / 2;
+  const int ch = on ? 2 * lane : 0;
+  const uint16_t* X = kv ? a.V : a.K;
+  const uint32_t d = *reinterpret_cast<const uint32_t*>(X + int64_t(z) * a.sL + (w.row0 + slot) * a.sT + head * a.sH + ch);
+  uint32_t* words = reinterpret_cast<uint32_t*>(rec + kv * CB);
+  const int xv = (ch / 16) * 2 + slot / 32;
+  uint32_t* vw = words + ((xv >> 2) * 64 + ((slot >> 2) & 3) * 16 + (ch & 15)) * 4 + (xv & 3);
+  uint32_t old0 = 0, old1 = 0;
+  if (kv) {
+    old0 = vw[0];
+    old1 = vw[4];
+  }
+  if (w.page < 0 || holders > 1) {
+    if (lane == 0) atomicOr(a.c.status, kBad);
+    return;
+  }
+  float x0, x1;
+  unpack2<BF>(d, x0, x1);
+  const bool ok = all_of<G / 2>(finite(x0) && finite(x1));
+  const Affine q(min_over<G / 2>(fminf(x0, x1)), max_over<G / 2>(fmaxf(x0, x1)));
+  const uint32_t c0 = ok ? q.code(x0) : 0u, c1 = ok ? q.code(x1) : 0u;
+  if (!ok && on) atomicOr(a.c.status, kNonfinite);
+  if (on && ch % G == 0)
+    reinterpret_cast<uint32_t*>(rec + 2 * CB + kv * paged_meta_bytes(D, G))[ch / G * kPage + slot] = ok ? q.bits : 0u;
+  if (kv) {
+    const int j = ((slot >> 4) & 1) * 4 + (slot & 3), sh = 4 * (j >> 1) + 16 * (j & 1);
+    if (on) {
+      vw[0] = (old0 & ~(15u << sh)) | c0 << sh;
+      vw[4] = (old1 & ~(15u << sh)) | c1 << sh;
+    }
+  } else {
+    int v = int(c0 << (4 * (lane & 3)) | c1 << (4 * (lane & 3) + 16));     // slots 2 (lane mod 4) and + 1
+    v |= __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);
+    v |= __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);
+    const int xk = (slot / 16) * KI + ch / 32;
+    if (on && (lane & 3) == 0) words[((xk >> 2) * 64 + (lane >> 2 & 3) * 16 + (slot & 15)) * 4 + (xk & 3)] = uint32_t(v);
+  }
+}
+
+// One workgroup quantizes the rows of one (page, layer, kv head): K and then
+// V, or one of them (a.parts == 2, where there are few pages).
+// Four lanes own a token row, D/4 channels each (with 16 lanes a row, loads
+// coalesce better, but a group's parameters, two divisions, are worked out in
+// four times as many lanes: 140 us instead of 96 for 76000 rows of 8 heads);
+// the codes go to LDS as bytes and come out as the words of the record's
+// layout.  A page that the rows fill only in part keeps its other rows: K
+// words belong to one row, V words hold 8 tokens and are merged with what is
+// there.  Memory-bound.
 template <int D, int G, int BF>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
-  constexpr int Q = D / 4;                         // channels of a lane
-  constexpr int LG = G / Q > 1 ? G / Q : 1;        // lanes of a group
-  constexpr int GQ = Q / G > 1 ? Q / G : 1;        // groups of a lane
-  constexpr int CB = paged_code_bytes(D), KI = D / 32;
-  constexpr int PITCH = D + 4;
+  constexpr int Q = D / 4;                               // channels of a lane
+  constexpr int LG = G / Q > 1 ? G / Q : 1;              // lanes of a group
+  constexpr int GQ = Q / G > 1 ? Q / G : 1, N = Q / GQ;  // groups of a lane, channels of each
+  constexpr int CB = paged_code_bytes(D), KI = D / 32, PITCH = D + 4;
   __shared__ __align__(16) uint8_t codes[kPage * PITCH];
   const PagedView& c = a.c;
   const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
-  const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
+  const int z = a.parts == 2 ? blockIdx.z >> 1 : blockIdx.z, layer = a.layer0 + z, head = blockIdx.y;
+  const int kv0 = a.parts == 2 ? blockIdx.z & 1 : 0, kv1 = a.parts == 2 ? kv0 : 1;
   if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
   const int stalled = *c.stalled;
   const PageWork w = page_work(c, a.r, blockIdx.x);
   if (w.seq < 0 || stalled) return;
   const int holders = c.refs[max(w.page, 0)];
-  const bool mine = slot >= w.lo && slot < w.hi;
-  // both rows are loaded before the page's holders are looked at
-  uint4 in[2][Q / 8];
-  const int64_t from = int64_t(blockIdx.z) * a.sL + (w.row0 + (mine ? slot : w.lo)) * a.sT + head * a.sH + q * Q;
-#pragma unroll
-  for (int i = 0; i < Q / 8; ++i) {
-    in[0][i] = reinterpret_cast<const uint4*>(a.K + from)[i];
-    in[1][i] = reinterpret_cast<const uint4*>(a.V + from)[i];
+  uint8_t* rec = paged_record_at(c, max(w.page, 0), layer, head);
+  if (w.hi - w.lo == 1) {
+    const int kv = kv0 + (tid >> 6);               // a wave each
+    if (kv <= kv1) write_row<D, G, BF>(a, w, rec, z, kv, holders);
+    return;
   }
+  // the rows are loaded before the page's holders are looked at; slots that
+  // are no rows of the call load the first's
+  const bool mine = slot >= w.lo && slot < w.hi;
+  const int64_t from = int64_t(z) * a.sL + (w.row0 + (mine ? slot : w.lo)) * a.sT + head * a.sH + q * Q;
+  uint4 in[Q / 8];
+#pragma unroll
+  for (int i = 0; i < Q / 8; ++i) in[i] = reinterpret_cast<const uint4*>((kv0 ? a.V : a.K) + from)[i];
   if (w.page < 0 || holders > 1) {
     if (tid == 0) atomicOr(c.status, kBad);
     return;
   }
-  uint8_t* rec = paged_record_at(c, w.page, layer, head);
   bool bad = false;
-#pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll 1
+  for (int kv = kv0; kv <= kv1; ++kv) {
+    uint32_t* meta = reinterpret_cast<uint32_t*>(rec + 2 * CB + kv * paged_meta_bytes(D, G));
     float x[Q];
 #pragma unroll
     for (int i = 0; i < Q / 8; ++i) {
-      const uint4 v = in[kv][i];
-      const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+      const uint32_t d[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (BF) {
-          x[8 * i + 2 * e] = __uint_as_float(d[e] << 16);
-          x[8 * i + 2 * e + 1] = __uint_as_float(d[e] & 0xFFFF0000u);
-        } else {
-          x[8 * i + 2 * e] = h2f(d[e] & 0xFFFFu);
-          x[8 * i + 2 * e + 1] = h2f(d[e] >> 16);
-        }
-      }
+      for (int e = 0; e < 4; ++e) unpack2<BF>(d[e], x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
     }
-    uint32_t* meta = reinterpret_cast<uint32_t*>(rec + 2 * CB + kv * paged_meta_bytes(D, G));
-    if (kv) __syncthreads();                       // K's codes have been read
+    if (kv < kv1) {                                      // V's row while K's is worked on
+#pragma unroll
+      for (int i = 0; i < Q / 8; ++i) in[i] = reinterpret_cast<const uint4*>(a.V + from)[i];
+    } else if (kv > kv0) {
+      __syncthreads();                                   // K's codes have been read
+    }
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
-      constexpr int N = Q / GQ;
       float mn = x[g * N], mx = mn, nan = 0.0f * mn;
 #pragma unroll
       for (int i = 1; i < N; ++i) {
         mn = fminf(mn, x[g * N + i]);
         mx = fmaxf(mx, x[g * N + i]);
-        nan = fmaf(x[g * N + i], 0.0f, nan);       // 0, or NaN once a value is not finite
+        nan = fmaf(x[g * N + i], 0.0f, nan);             // 0, or NaN once a value is not finite
       }
-#pragma unroll
-      for (int m = 1; m < LG; m <<= 1) {
-        mn = fminf(mn, __shfl_xor(mn, m));
-        mx = fmaxf(mx, __shfl_xor(mx, m));
-        nan += __shfl_xor(nan, m);
-      }
-      const bool finite = nan == 0.0f;
-      bad |= mine && !finite;
-      // zero and scale as fp16, saturated; codes against the stored pair
-      const uint32_t zb = f2h(fminf(fmaxf(mn, -65504.0f), 65504.0f) + 0.0f);
-      const float z = h2f(zb);
-      const uint32_t sb = f2h(fminf(fmaxf((mx - z) / 15.0f, 0.0f), 65504.0f));
-      const float sc = h2f(sb), inv = sc > 0.0f ? 1.0f / sc : 0.0f;
+      const bool ok = all_of<LG>(nan == 0.0f);
+      const Affine p(LG > 1 ? min_over<LG>(mn) : mn, LG > 1 ? max_over<LG>(mx) : mx);
+      bad |= mine && !ok;
 #pragma unroll
       for (int i = 0; i < N; i += 4) {
         uint32_t pack = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float r = fminf(fmaxf(__builtin_rintf((x[g * N + i + e] - z) * inv), 0.0f), 15.0f);
-          pack |= uint32_t(r) << (8 * e);
-        }
-        *reinterpret_cast<uint32_t*>(codes + slot * PITCH + q * Q + g * N + i) = finite ? pack : 0u;
+        for (int e = 0; e < 4; ++e) pack |= p.code(x[g * N + i + e]) << (8 * e);
+        *reinterpret_cast<uint32_t*>(codes + slot * PITCH + q * Q + g * N + i) = ok ? pack : 0u;
       }
-      if (mine && (LG == 1 || q % LG == 0)) meta[((q * Q) / G + g) * kPage + slot] = finite ? sb | zb << 16 : 0u;
+      if (mine && q % LG == 0) meta[((q * Q) / G + g) * kPage + slot] = ok ? p.bits : 0u;
     }
     __syncthreads();
     uint32_t* words = reinterpret_cast<uint32_t*>(rec + kv * CB);
-    const int first = w.lo, last = w.hi;
     for (int i = tid; i < kPage * D / 8; i += 256) {
       const int lane = (i >> 2) & 63, x4 = 4 * (i >> 8) + (i & 3);
       if (kv == 0) {
         const int t = 16 * (x4 / KI) + (lane & 15);
-        if (t < first || t >= last) continue;
+        if (t < w.lo || t >= w.hi) continue;
         const uint32_t* p = reinterpret_cast<const uint32_t*>(codes + t * PITCH + 32 * (x4 % KI) + 8 * (lane >> 4));
         uint32_t v = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v |= ((p[j >> 2] >> (8 * (j & 3))) & 15u) << (4 * (j >> 1) + 16 * (j & 1));
         words[i] = v;
       } else {
-        const int ch = 16 * (x4 >> 1) + (lane & 15), t0 = 32 * (x4 & 1) + 4 * (lane >> 4);
+        const int vch = 16 * (x4 >> 1) + (lane & 15), t0 = 32 * (x4 & 1) + 4 * (lane >> 4);
         uint32_t v = 0, mask = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int t = t0 + 16 * (j >> 2) + (j & 3), sh = 4 * (j >> 1) + 16 * (j & 1);
-          if (t >= first && t < last) {
-            v |= uint32_t(codes[t * PITCH + ch]) << sh;
-            mask |= 15u << sh;
-          }
+          const bool in_call = uint32_t(t - w.lo) < uint32_t(w.hi - w.lo);
+          v |= (in_call ? uint32_t(codes[t * PITCH + vch]) : 0u) << sh;
+          mask |= (in_call ? 15u : 0u) << sh;
         }
         if (mask == ~0u) words[i] = v;
         else if (mask) words[i] = (words[i] & ~mask) | v;
@@ -655,8 +754,12 @@ static void write_of(const PagedWriteArgs& a, dim3 grid, hipStream_t s) {
   else hipLaunchKernelGGL((paged_write_kernel<D, G, 0>), grid, dim3(256), 0, s, a);
 }
 
-int launch_paged_write(const PagedWriteArgs& a, hipStream_t s) {
-  const dim3 grid(unsigned(touched_bound(a.r)), unsigned(a.c.n_kv_heads), unsigned(a.layers));
+int launch_paged_write(PagedWriteArgs a, hipStream_t s) {
+  // K and V in workgroups of their own where there are few: 2048 rows of 8
+  // heads 7.8 us, 9.1 together; 76000 rows 110 us, 95 together
+  const int64_t bound = touched_bound(a.r);
+  a.parts = bound * a.c.n_kv_heads * a.layers < 2048 ? 2 : 1;
+  const dim3 grid(unsigned(bound), unsigned(a.c.n_kv_heads), unsigned(a.parts * a.layers));
   if (a.c.dim == 128) {
     if (a.c.group == 128) write_of<128, 128>(a, grid, s);
     else if (a.c.group == 64) write_of<128, 64>(a, grid, s);
