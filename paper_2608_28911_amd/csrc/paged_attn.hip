@@ -232,9 +232,13 @@ __device__ inline void put_row(const PagedAttnArgs& a, const Tile& tl, int head,
 template <int D>
 constexpr int partial_floats(int rows) { return rows * (D + 4); }
 
-template <int D, int G, int NR, int NW>
+// SHARE: every wave has rows of its own and all walk the tile's pages together,
+// each decoding a part of a page's codes into LDS for the others: a quarter of
+// the decoding, for calls whose tiles fill the chip.  Otherwise the waves share
+// rows and take pages in turn.
+template <int D, int G, int NR, int NW, bool SHARE>
 __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a) {
-  constexpr int NK = D / 32, NC = D / 16, NG = D / G, KG = G / 32, CG = G / 16, ROWS = 16 * NR;
+  constexpr int NK = D / 32, NC = D / 16, NG = D / G, KG = G / 32, CG = G / 16, ROWS = 16 * NR * (SHARE ? NW : 1);
   constexpr int CB = paged_code_bytes(D), NP = D / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const PagedView& c = a.c;
@@ -245,17 +249,17 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 
   // the rows' queries, and behind them the wave's first record: in flight together
   uint4 qw[NR][NK];
-  const int m0 = tl.len - tl.count;
+  const int m0 = tl.len - tl.count, first = tl.first + (SHARE ? 16 * NR * wave : 0);   // the wave's first row
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const int row = tl.first + 16 * r + n < tl.rows ? tl.first + 16 * r + n : tl.first;
+    const int row = first + 16 * r + n < tl.rows ? first + 16 * r + n : tl.first;
     const int i = int(uint32_t(row) / uint32_t(a.gqa)), g = row - i * a.gqa;
     const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.sT + int64_t(head * a.gqa + g) * a.sH + 8 * kg;
 #pragma unroll
     for (int k = 0; k < NK; ++k) qw[r][k] = *reinterpret_cast<const uint4*>(src + 32 * k);
   }
-  // the tile's first row sees the least: pages up to here need no mask
-  const int all_see = m0 + tl.first / a.gqa;
+  // the first row sees the least: pages up to here need no mask
+  const int all_see = m0 + int(uint32_t(first) / uint32_t(a.gqa));
   const int each = int(uint32_t(tl.pages + tl.splits - 1) / uint32_t(tl.splits));
   const int p0 = split * each, p1 = min(p0 + each, tl.pages);
   const int32_t* table = c.table + int64_t(tl.seq) * c.seq_pages;
@@ -270,12 +274,48 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   auto load = [&](const __amdgpu_buffer_rsrc_t& rs, int offset) {
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + offset, 0, 0));
   };
-  // Metadata goes through LDS, a region for each wave: 16 lanes share a token's
-  __shared__ __align__(16) uint4 sm_meta[NW][32 * NG];
-  constexpr int MV = (32 * NG + 63) / 64;          // 16-byte loads of it
-  uint4 kw[NP], vw[NP], mw[MV];
-  int page = page_at(p0 + wave), next = page_at(p0 + wave + NW);
-  {
+  // Metadata goes through LDS (16 lanes share a token's), a region for each
+  // wave; with SHARE a region for each of two pages, and the operands with it
+  constexpr int META = 32 * NG, MV = (META + 63) / 64;   // 16-byte words of it, and loads of a wave
+  constexpr int FK = SHARE ? 4 * NK : 1, FV = SHARE ? 2 * NC : 1;
+  __shared__ __align__(16) uint4 sm_meta[SHARE ? 2 : NW][META];
+  __shared__ __align__(16) half8v sm_k[SHARE ? 2 : 1][FK][64], sm_v[SHARE ? 2 : 1][FV][64];
+  // with SHARE a wave decodes pieces wave, wave + NW, ... of K's and then V's
+  constexpr int MINE = SHARE ? 2 * NP / NW : 1;
+  static_assert(!SHARE || (2 * NP % NW == 0 && NW >= 2), "pieces of a page");
+  uint4 kw[SHARE ? 1 : NP], vw[SHARE ? 1 : NP], mw[SHARE ? 1 : MV], pw[MINE];
+  int page, next;
+  auto load_shared = [&](const __amdgpu_buffer_rsrc_t& rs) {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) pw[i] = load(rs, 1024 * (wave + NW * i));
+    if (wave < MV) mw[0] = load(rs, 2 * CB + 1024 * wave);
+  };
+  // what was loaded of page p to its place; `have` tokens of the sequence are cached
+  auto stage_shared = [&](int p, int have) {
+    const int buf = p & 1;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int piece = wave + NW * i;
+      half8v* to = piece < NP ? &sm_k[buf][4 * piece & (FK - 1)][lane] : &sm_v[buf][4 * (piece - NP) & (FV - 1)][lane];
+      const uint32_t d[4] = {pw[i].x, pw[i].y, pw[i].z, pw[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[64 * e] = codes8(d[e]);
+    }
+    if (wave < MV && 64 * wave + lane < META) {
+      const int at = 64 * wave + lane, t = p * kPage + 4 * (at & 15);
+      uint32_t m[4] = {mw[0].x, mw[0].y, mw[0].z, mw[0].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = at < 16 * NG || t + e < have ? m[e] : 0u;
+      sm_meta[buf][at] = make_uint4(m[0], m[1], m[2], m[3]);
+    }
+  };
+  if constexpr (SHARE) {
+    page = page_at(0);
+    next = page_at(1);
+    load_shared(record(page));
+  } else {
+    page = page_at(p0 + wave);
+    next = page_at(p0 + wave + NW);
     const auto rs = record(page);
 #pragma unroll
     for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
@@ -291,7 +331,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   float qs[NR][NG], cf[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const bool valid = tl.first + 16 * r + n < tl.rows;
+    const bool valid = first + 16 * r + n < tl.rows;
     uint32_t d[4 * NK];
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
@@ -344,31 +384,54 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     for (int ct = 0; ct < NC; ++ct) o[r][ct] = float4v{0, 0, 0, 0};
   }
 
-  for (int p = p0 + wave; p < p1; p += NW) {
+  if constexpr (SHARE) {
+    stage_shared(0, page < 0 ? 0 : tl.len);
+    load_shared(record(next));
+  }
+  // pages that the wave's last row sees (SHARE: it then only decodes)
+  const int last_seen = m0 + int(uint32_t(min(first + 16 * NR, tl.rows) - 1) / uint32_t(a.gqa));
+  for (int p = SHARE ? 0 : p0 + wave; p < p1; p += SHARE ? 1 : NW) {
     const auto rs = record(next);
     const int have = page < 0 ? 0 : tl.len;        // tokens of a missing page are past the end
-    page = next;
-    next = page_at(p + 2 * NW);
-    // a lane holds 4 tokens of a group, first K's groups, then V's.  V's for
-    // tokens past the sequence's end, which may be anything, become 0; the
-    // largest V scale of the others enters the softmax's reference
     uint32_t smax = 0;
-#pragma unroll
-    for (int i = 0; i < MV; ++i) {
-      const int at = 64 * i + lane, t = p * kPage + 4 * (at & 15);
-      uint32_t m[4] = {mw[i].x, mw[i].y, mw[i].z, mw[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (at >= 16 * NG) m[e] = t + e < have ? m[e] : 0u;
-        smax = max(smax, at >= 16 * NG && at < 32 * NG ? m[e] & 0xFFFFu : 0u);
+    const uint4* kmeta;                            // [group][tile][4 tokens of kg]
+    if constexpr (SHARE) {
+      __syncthreads();                             // page p is staged, page p - 1 has been used
+      if (p + 1 < p1) {
+        const int after = page_at(p + 2);
+        stage_shared(p + 1, next < 0 ? 0 : tl.len);
+        load_shared(record(after));
+        page = next;
+        next = after;
       }
-      if (32 * NG % 64 == 0 || at < 32 * NG) sm_meta[wave][at] = make_uint4(m[0], m[1], m[2], m[3]);
+      if (first >= tl.rows || p * kPage > last_seen) continue;
+      kmeta = sm_meta[p & 1] + kg;
+      const uint4 m = sm_meta[p & 1][16 * NG + (lane & (16 * NG - 1))];
+      smax = max(max(m.x & 0xFFFFu, m.y & 0xFFFFu), max(m.z & 0xFFFFu, m.w & 0xFFFFu));
+    } else {
+      page = next;
+      next = page_at(p + 2 * NW);
+      // a lane holds 4 tokens of a group, first K's groups, then V's.  V's for
+      // tokens past the sequence's end, which may be anything, become 0; the
+      // largest V scale of the others enters the softmax's reference
+#pragma unroll
+      for (int i = 0; i < MV; ++i) {
+        const int at = 64 * i + lane, t = p * kPage + 4 * (at & 15);
+        uint32_t m[4] = {mw[i].x, mw[i].y, mw[i].z, mw[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (at >= 16 * NG) m[e] = t + e < have ? m[e] : 0u;
+          smax = max(smax, at >= 16 * NG && at < META ? m[e] & 0xFFFFu : 0u);
+        }
+        if (META % 64 == 0 || at < META) sm_meta[wave][at] = make_uint4(m[0], m[1], m[2], m[3]);
+      }
+      wave_order();
+      kmeta = sm_meta[wave] + kg;
     }
-    wave_order();
-    const uint4* kmeta = sm_meta[wave] + kg;       // [group][tile][4 tokens of kg]
     const uint4* vmeta = kmeta + 16 * NG;
 
-    // scores
+    // scores (a wave with matrix instructions to issue goes first: 2 to 8 %)
+    __builtin_amdgcn_s_setprio(1);
     float4v x[NR][4];
     const uint32_t* kd = reinterpret_cast<const uint32_t*>(kw);
 #pragma unroll
@@ -380,7 +443,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
         for (int r = 0; r < NR; ++r) acc[r] = float4v{0, 0, 0, 0};
 #pragma unroll
         for (int k = j * KG; k < (j + 1) * KG; ++k) {
-          const half8v A = codes8(kd[tt * NK + k]);
+          const half8v A = SHARE ? sm_k[p & 1][(tt * NK + k) & (FK - 1)][lane] : codes8(kd[SHARE ? 0 : tt * NK + k]);
 #pragma unroll
           for (int r = 0; r < NR; ++r) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, qf[r][k], acc[r], 0, 0, 0);
         }
@@ -391,22 +454,25 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float s = lo16(m[e]), z = hi16(m[e]);
-            const float y = j == 0 ? z * qs[r][j] : fmaf(z, qs[r][j], x[r][tt][e]);
+            const float y = fmaf(z, qs[r][j], j == 0 ? 0.0f : x[r][tt][e]);   // (from the half as it is)
             x[r][tt][e] = fmaf(s, acc[r][e], y);
           }
       }
       if (NG > 1) __builtin_amdgcn_sched_barrier(0);   // else the metadata of every tile is read at once, and spilled
     }
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (!SHARE) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
+      for (int i = 0; i < NP; ++i) kw[i] = load(rs, 1024 * i);
 #pragma unroll
-    for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
+      for (int i = 0; i < MV; ++i) mw[i] = load(rs, 2 * CB + 1024 * i);
+    }
     const int t0 = p * kPage + 4 * kg;             // the lane's first token
     if (p * kPage + kPage - 1 > all_see || have == 0) {   // not every row sees every token
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         // the last token the row sees; worked out here, not kept in a register
-        int row = tl.first + 16 * r + n;
+        int row = first + 16 * r + n;
         __asm__ volatile("" : "+v"(row));
         const int seen = m0 + int(uint32_t(min(row, tl.rows - 1)) / uint32_t(a.gqa));
 #pragma unroll
@@ -487,18 +553,22 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 #pragma unroll
         for (int r = 0; r < NR; ++r) ws[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, wf[r][st], ws[r], 0, 0, 0);
       // values
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ct = j * CG; ct < (j + 1) * CG; ++ct)
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          const half8v A = codes8(vd[ct * 2 + st]);
+          const half8v A = SHARE ? sm_v[p & 1][(ct * 2 + st) & (FV - 1)][lane] : codes8(vd[SHARE ? 0 : ct * 2 + st]);
 #pragma unroll
           for (int r = 0; r < NR; ++r) o[r][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, wf[r][st], o[r][ct], 0, 0, 0);
         }
     }
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (!SHARE) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
-    wave_order();                                  // the metadata has been read
+      for (int i = 0; i < NP; ++i) vw[i] = load(rs, CB + 1024 * i);
+      wave_order();                                // the metadata has been read
+    }
   }
 
   // the waves' states merge in LDS, 16 rows at a time; then the tile's output,
@@ -506,6 +576,22 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   // (the lane's number made anew: kept over the loop it would be spilled)
   const int lane2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)), tid = 64 * wave + lane2;
   const int n2 = lane2 & 15, kg2 = lane2 >> 4;
+  if constexpr (SHARE) {                           // the wave's rows are whole
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const float L = row_sum(l[r]);
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        const float w = NG == 1 ? ws[r][0] : __shfl(ws[r][0], 16 * j + n2);
+        az[r][j] = fmaf(w, -7.5f * kSum, row_sum(az[r][j]));
+      }
+      if (first + 16 * r + n2 >= tl.rows) continue;
+#pragma unroll
+      for (int ct = 0; ct < NC; ++ct)
+        put_row<D>(a, tl, head, first + 16 * r + n2, 16 * ct + 4 * kg2, M[r], L, o[r][ct] * kCode + az[r][ct / CG]);
+    }
+    return;
+  }
   constexpr int PITCH = D + 4, LPR = D / 4, NT = 64 * NW;   // LPR: threads of an output row
   __shared__ float sm_m[NW][ROWS], sm_l[NW][ROWS];
   __shared__ __align__(16) float sm_o[NW][16][PITCH];
@@ -650,21 +736,23 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   }
 }
 
-template <int D, int G, int NR, int NW>
+template <int D, int G, int NR, int NW, bool SHARE = false>
 int launch(PagedAttnArgs a, hipStream_t s) {
   // tiles of the call: a whole tile's rows each, and one more a sequence
-  const int64_t whole = a.r.n_rows * ((a.gqa + 16 * NR - 1) / (16 * NR));
-  int64_t tiles = a.r.n_rows * a.gqa / (16 * NR) + a.r.n_seqs;
+  constexpr int ROWS = 16 * NR * (SHARE ? NW : 1);
+  const int64_t whole = a.r.n_rows * ((a.gqa + ROWS - 1) / ROWS);
+  int64_t tiles = a.r.n_rows * a.gqa / ROWS + a.r.n_seqs;
   if (tiles > whole) tiles = whole;
   const int64_t units = tiles * a.c.n_kv_heads;
   if (units >= (int64_t(1) << 22)) return -2;      // a grid's threads are counted in 32 bits
   int64_t wanted = kSlots * 4 / NW / a.c.n_kv_heads;
   if (wanted < 1) wanted = 1;
+  if (SHARE) wanted = 1;                           // no tile is split
   a.target = int(wanted);
   // every tile, and a share of the wanted ones where pages are split
   int64_t grid = tiles + wanted;
-  if (a.c.seq_pages <= kWhole) grid = tiles;
-  hipLaunchKernelGGL((paged_attn_kernel<D, G, NR, NW>), dim3(unsigned(grid * a.c.n_kv_heads)), dim3(64 * NW), 0, s, a);
+  if (SHARE || a.c.seq_pages <= kWhole) grid = tiles;
+  hipLaunchKernelGGL((paged_attn_kernel<D, G, NR, NW, SHARE>), dim3(unsigned(grid * a.c.n_kv_heads)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
@@ -674,11 +762,17 @@ int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
   // A workgroup of 8 waves for a single sequence: half as many splits to join
   // (one token over 32k tokens 14.9 us, with 4 waves 17.7); else of 4, two of
   // which hide each other's beginnings and ends (8 x 4k tokens 14.1, 21.5)
-  if (rows <= 16 && a.r.n_seqs == 1) return launch<D, G, 1, 8>(a, s);
+  // or where a sequence holds few pages at most (2k tokens 9.4, with 8 10.4)
+  if (rows <= 16 && a.r.n_seqs == 1 && a.c.seq_pages > 64) return launch<D, G, 1, 8>(a, s);
   if (rows <= 16) return launch<D, G, 1, 4>(a, s);
   // as above: 5 tokens of 4 x 32k, with 8 waves 35.5 us, with 4 42.6; 8 chunks
   // of 64 tokens, which fill the chip, 65.5 and 56.7
   if (rows * a.r.n_seqs * a.c.n_kv_heads <= 32 * 128) return launch<D, G, 2, 8>(a, s);
+  // Decoding shared by a workgroup's waves, which make a tile of four times the
+  // rows, where such tiles give every compute unit two: 4 prompts of 1024
+  // tokens 79 us, 108 apart; a 2048-token chunk over 16k (512 workgroups) 736
+  // and 748; but 8 chunks of 64 tokens (128 workgroups) 126 and 59
+  if ((a.r.n_rows * a.gqa / 128 + a.r.n_seqs) * a.c.n_kv_heads >= 512) return launch<D, G, 2, 4, true>(a, s);
   return launch<D, G, 2, 4>(a, s);
 }
 
