@@ -111,7 +111,8 @@ struct Kept {
 };
 __device__ inline void keep(Kept& s, uint32_t h, uint32_t l, int lane) {   // h, l uniform
   const int at = __popcll(__ballot(s.above(h, l)));       // kept keys above it come first
-  const uint32_t uh = __shfl_up(s.hi, 1), ul = __shfl_up(s.lo, 1);
+  // the lane below's keys: a DPP move along the wave
+  const uint32_t uh = __builtin_amdgcn_mov_dpp(int(s.hi), 0x138, 0xF, 0xF, true), ul = __builtin_amdgcn_mov_dpp(int(s.lo), 0x138, 0xF, 0xF, true);
   if (lane == at) {
     s.hi = h;
     s.lo = l;
@@ -137,12 +138,12 @@ __device__ inline float logit_of(uint32_t order) {
   return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
-// The k-th largest of the lanes' orders (its upper 24 bits): as many lanes hold
+// The k-th largest of the lanes' orders (its upper 16 bits): as many lanes hold
 // a logit that is no smaller, so a row's k likeliest are not below it.
 __device__ inline uint32_t kth_order(uint32_t h, int k) {
   uint32_t t = 0;
 #pragma unroll
-  for (int b = 31; b >= 8; --b)
+  for (int b = 31; b >= 16; --b)
     if (__popcll(__ballot(h >= (t | 1u << b))) >= k) t |= 1u << b;
   return t;
 }
@@ -150,24 +151,30 @@ __device__ inline uint32_t kth_order(uint32_t h, int k) {
 // Partial of one split of a row: m, S, T, then the kept keys.
 __host__ __device__ constexpr int partial_words(int top) { return 4 + 2 * top; }
 
-__device__ inline void finish(const TokenArgs& a, int64_t row, const Sums& s) {
+// A row's target and its logit.
+struct Given { int64_t target; float x; };
+__device__ inline Given given(const TokenArgs& a, int64_t row) {
+  Given g = {-1, 0.0f};
+  if (!a.logp) return g;
   const int b = int(row / a.T);
   const int64_t t = row - b * a.T;
+  g.target = a.targets[b * a.t_batch + t * a.t_token];
+  if (g.target >= 0 && g.target < a.vocab) {
+    const char* p = static_cast<const char*>(a.x) + (b * a.s_batch + t * a.s_token) * (a.dtype == 2 ? 4 : 2);
+    g.x = a.dtype == 2 ? load1<2>(p, g.target) : a.dtype == 1 ? load1<1>(p, g.target) : load1<0>(p, g.target);
+  }
+  return g;
+}
+
+__device__ inline void finish(const TokenArgs& a, int64_t row, const Given& g, const Sums& s) {
+  const int b = int(row / a.T);
+  const int64_t t = row - b * a.T, at = b * a.o_batch + t * a.o_token;
   const float ln = __builtin_logf(s.S);
-  const int64_t at = b * a.o_batch + t * a.o_token;
   const bool fine = s.S > 0.0f && s.S < INFINITY;         // not NaN either
   if (a.entropy) a.entropy[at] = fine ? ln - s.T / s.S : NAN;
   if (a.logp) {
-    const int64_t target = a.targets[b * a.t_batch + t * a.t_token];
-    float v = NAN;
-    if (target == -1) {
-      v = 0.0f;
-    } else if (target >= 0 && target < a.vocab && fine) {
-      const char* p = static_cast<const char*>(a.x) + (b * a.s_batch + t * a.s_token) * (a.dtype == 2 ? 4 : 2);
-      const float x = a.dtype == 2 ? load1<2>(p, target) : a.dtype == 1 ? load1<1>(p, target) : load1<0>(p, target);
-      v = (x - s.m) - ln;
-    }
-    a.logp[at] = a.negate && target != -1 ? -v : v;
+    const float v = g.target >= 0 && g.target < a.vocab && fine ? (g.x - s.m) - ln : NAN;
+    a.logp[at] = g.target == -1 ? 0.0f : a.negate ? -v : v;
   }
 }
 
@@ -273,6 +280,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
   }
   __syncthreads();
   if (wave != 0) return;
+  const Given g = a.nsplit == 1 ? given(a, row) : Given{-1, 0.0f};
   s = join_wave(lane < WAVES ? sm[lane] : Sums{kFloor, 0.0f, 0.0f});
   if constexpr (TOP) {
     for (int i = k; i < WAVES * k; i += 64) {              // the other waves' keys into wave 0's
@@ -294,17 +302,27 @@ __global__ __launch_bounds__(64 * WAVES) void token_logprobs_kernel(TokenArgs a)
     }
     return;
   }
-  if (lane == 0) finish(a, row, s);
+  if (lane == 0) finish(a, row, g, s);
   if (TOP && lane < k) finish_top(a, row, s, kept.hi, kept.lo, lane);
 }
 
-// The splits of a row joined, a wave each.
+// The splits of a row joined, a wave each: everything it needs is loaded first.
 __global__ __launch_bounds__(64) void token_merge_kernel(TokenArgs a) {
   const int lane = threadIdx.x, k = a.top;
   const int64_t row = blockIdx.x;
   const uint32_t* p = reinterpret_cast<const uint32_t*>(a.ws) + row * a.nsplit * partial_words(k);
+  auto key = [&](int at, uint32_t& h, uint32_t& l) {
+    const int sp = at / max(k, 1), j = at - sp * k;
+    const bool valid = at < a.nsplit * k;
+    const uint32_t* q = p + (valid ? sp * partial_words(k) + 4 + 2 * j : 0);
+    h = q[0];
+    l = q[1];
+    if (!valid) h = l = 0;
+  };
+  uint32_t h, l;
+  key(lane, h, l);
+  const Given g = given(a, row);
   Sums s = {kFloor, 0.0f, 0.0f};
-  Kept kept = {0u, 0u};
   for (int i = lane; i < a.nsplit; i += 64) {
     const uint32_t* q = p + i * partial_words(k);
     Sums t = {__uint_as_float(q[0]), __uint_as_float(q[1]), __uint_as_float(q[2])};
@@ -315,14 +333,13 @@ __global__ __launch_bounds__(64) void token_merge_kernel(TokenArgs a) {
     s.T += t.T;
   }
   s = join_wave(s);
-  if (lane == 0) finish(a, row, s);
+  if (lane == 0) finish(a, row, g, s);
   if (k == 0) return;
+  Kept kept = {0u, 0u};
+  const uint32_t least = kth_order(h, k);          // of the first 64 keys, which the rest cannot lower
   for (int i = 0; i < a.nsplit * k; i += 64) {
-    const int at = i + lane, sp = at / k, j = at - sp * k;
-    const bool valid = at < a.nsplit * k;
-    const uint32_t* q = p + sp * partial_words(k) + 4 + 2 * j;
-    const uint32_t h = valid ? q[0] : 0u, l = valid ? q[1] : 0u;
-    keep_all(kept, valid, h, l, k, lane);
+    if (i) key(i + lane, h, l);
+    keep_all(kept, h != 0 && h >= least, h, l, k, lane);
   }
   if (lane < k) finish_top(a, row, s, kept.hi, kept.lo, lane);
 }

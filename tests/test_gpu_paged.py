@@ -90,7 +90,7 @@ def stored(pool, table, s, n, layer, head, d, g):
     return [tuple(np.concatenate([p[i] for p in parts])[:n] for i in range(3)) if parts else None for parts in out]
 
 
-def check_attn(cache, lens, counts, q, out, lse, scale, layer=0):
+def check_attn(cache, lens, counts, q, out, lse, scale, layer=0, only=None):
     c, pool, table = cache.cfg, pool_of(cache), cache.table.cpu().numpy()
     d, g, gq = c.head_dim, c.group, c.n_q_heads // c.n_kv_heads
     eps = {2.0 ** -10: 2.0 ** -11, 2.0 ** -7: 2.0 ** -8}[float(__import__("torch").finfo(out.dtype).eps)]
@@ -103,6 +103,8 @@ def check_attn(cache, lens, counts, q, out, lse, scale, layer=0):
             for i in range(m):
                 seen = n - m + i + 1
                 for h in range(head * gq, (head + 1) * gq):
+                    if only is not None and not only(at + i, h):
+                        continue
                     o, l = out[at + i, h], lse[at + i, h]
                     if seen <= 0:
                         assert not o.any() and l == -np.inf
@@ -238,6 +240,44 @@ def test_attn_several_tokens(d, g, counts, gqa):
     q = rows(rng, (n, 2 * gqa, d), torch.float16) * 0.3
     out, lse = c.attn(0, q, starts_of(counts), with_lse=True, scale=0.2)
     check_attn(c, lens, counts, q, out, lse, 0.2)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d,g", [(128, 128), (128, 64), (128, 32), (64, 64), (64, 32)])
+def test_attn_prompts_that_fill_the_chip(d, g, bf16):
+    """Tiles of 128 rows, whose waves decode pages for each other: ragged prompts
+    and chunks, among them one token, an empty sequence, one shorter than its
+    chunk, and pages that are missing; checked at every 37th (row, head) and at
+    the ends."""
+    import torch
+    rng = np.random.default_rng(d + g)
+    h, gq = 8, 8
+    c = make(h=h, hq=h * gq, d=d, g=g, n_pages=60, seqs=6, seq_pages=16)
+    lens, counts = [500, 1, 0, 900, 30, 333], [500, 1, 0, 300, 70, 200]
+    fill(c, lens, rng)
+    n = sum(counts)
+    q = (rows(rng, (n, h * gq, d), torch.float32) * 0.3).to(torch.bfloat16 if bf16 else torch.float16)
+    out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
+    ends = {0, 499, 500, 501, 801 - 1, 801, 840, 841, 870, 871, n - 1}
+    check_attn(c, lens, counts, q, out, lse, d ** -0.5, only=lambda t, hh: (t * h * gq + hh) % 37 == 0 and t % 5 == 0 or t in ends and hh in (0, 63))
+    table = c.table.clone()
+    table[3, 2], table[5, 0] = -1, -1                    # 64 tokens of one, the first 64 of another
+    c.assign(c.lens.clone(), table)
+    got, gl = c.attn(0, q, starts_of(counts), with_lse=True)
+    assert torch.equal(got[:501], out[:501])
+    pool, table = pool_of(c), table.cpu().numpy()
+    for t, s, pos in ((501, 3, 600), (800, 3, 899), (871, 5, 133), (n - 1, 5, 332)):
+        k, v = [], []
+        for i in range(pos // 64 + 1):
+            if table[s, i] >= 0:
+                a, b = R.values(pool[table[s, i], 0, 3], d, g)
+                m = min(64, pos + 1 - 64 * i)
+                k.append(a[:m])
+                v.append(b[:m])
+        k, v = np.concatenate(k), np.concatenate(v)
+        want, wl, _ = R.attend(np_of(q[t, 8 * 3 + 5]).astype(np.float64), k, v, len(k), d ** -0.5)
+        # the tolerance of a row above, with everything at its largest
+        assert np.abs(np_of(got[t, 29]) - want).max() <= 2.0 ** -7 * np.abs(v).max() and abs(float(gl[t, 29]) - wl) <= 1e-2
 
 
 def test_attn_rows_before_the_first_token():
