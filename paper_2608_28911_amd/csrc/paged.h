@@ -93,6 +93,12 @@ __device__ inline SeqRows seq_rows(const PagedRows& r, int s) {
   return {a, b - a};
 }
 
+// Starts that descend, or pass the rows there are.
+__device__ inline bool starts_bad(const PagedRows& r, int s) {
+  const int32_t a = r.starts[s], b = r.starts[s + 1];
+  return a < 0 || b < a || b > r.n_rows;
+}
+
 // Which sequence's tile a flat index names, where sequence s has tiles(s) of
 // them: the whole wave counts 64 sequences at a time.  -1 past the last.
 template <class F>

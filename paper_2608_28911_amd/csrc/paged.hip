@@ -378,10 +378,8 @@ int64_t touched_bound(const PagedRows& r) {
 
 // Starts that are no partition of rows, or rows before the first token.
 __device__ inline void check_rows(const PagedView& c, const PagedRows& r) {
-  for (int s = threadIdx.x; s < r.n_seqs; s += blockDim.x) {
-    const int32_t a = r.starts[s], b = r.starts[s + 1];
-    if (a < 0 || b < a || b > r.n_rows || b - a > c.lens[s]) atomicOr(c.status, kBad);
-  }
+  for (int s = threadIdx.x; s < r.n_seqs; s += blockDim.x)
+    if (starts_bad(r, s) || r.starts[s + 1] - r.starts[s] > c.lens[s]) atomicOr(c.status, kBad);
 }
 
 // Group parameters as fp16, saturated, and a code against the stored pair.

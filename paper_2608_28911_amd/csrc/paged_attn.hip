@@ -243,6 +243,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const PagedView& c = a.c;
   const int head = blockIdx.x % c.n_kv_heads;
+  if (blockIdx.x == gridDim.x - 1)                 // (the last workgroup: seldom one with a tile)
+    for (int s = threadIdx.x; s < a.r.n_seqs; s += 64 * NW)
+      if (starts_bad(a.r, s)) atomicOr(c.status, 4);
   const Tile tl = tile_of<ROWS>(a, blockIdx.x / c.n_kv_heads, lane);
   const int split = tl.split;
   if (tl.seq < 0 || split >= tl.splits) return;

@@ -359,6 +359,31 @@ def test_attn_long_sequence_and_many_splits():
         check_attn(c, lens, counts, q, out, lse, 128 ** -0.5)
 
 
+def test_many_sequences():
+    """More sequences than a wave has lanes, some empty, some without a row in
+    the call: writes, reads and attention of one and of several tokens."""
+    import torch
+    rng = np.random.default_rng(13)
+    n = 150
+    lens = [int(x) for x in rng.integers(0, 200, n)]
+    lens[70], lens[149] = 1500, 700
+    c = make(h=1, hq=4, d=64, g=32, n_pages=700, seqs=n, seq_pages=24)
+    fill(c, lens, rng)
+    back = c.read(0, starts_of(lens), sum(lens), dtype=torch.float32)[0]
+    pool, table = pool_of(c), c.table.cpu().numpy()
+    at = 0
+    for s, m in enumerate(lens):
+        for t in {0, m // 2, m - 1} if m else ():
+            want = R.values(pool[table[s, t // 64], 0, 0], 64, 32)[0][t % 64]
+            assert np.array_equal(back[at + t, 0].cpu().numpy(), want.astype(np.float32))
+        at += m
+    for counts in ([1] * n, [int(rng.integers(0, 2)) for _ in lens], [int(rng.integers(0, min(m, 40) + 1)) for m in lens]):
+        q = rows(rng, (sum(counts), 4, 64), torch.float16) * 0.3
+        out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
+        check_attn(c, lens, counts, q, out, lse, 64 ** -0.5, only=lambda t, h: (t + h) % 7 == 0)
+    assert c.status() == 0
+
+
 # ------------------------------------------------------------------ pages --
 
 def assert_tables(c, m):
@@ -435,6 +460,31 @@ def test_random_page_calls(n_pages, seqs, seq_pages, seed):
         live = np.array(m.refs()) == 0
         want[live] = pool_of(c)[live]
         assert c.status() == (R.NO_PAGES if failed else 0)
+
+
+@pytest.mark.parametrize("n_pages,seqs,seq_pages", [(70001, 3, 30000), (5000, 1024, 9)])
+def test_page_calls_at_the_limits(n_pages, seqs, seq_pages):
+    """Bitmaps of more words than a workgroup has threads; every slot in use."""
+    rng = np.random.default_rng(n_pages)
+    c = make(h=1, hq=1, d=64, g=64, n_pages=n_pages, seqs=seqs, seq_pages=seq_pages)
+    m = R.Pages(n_pages, seqs, seq_pages)
+    for most in (seq_pages * 40, 1, 1):
+        n = rng.integers(0, most + 1, seqs).tolist()
+        c.reserve(ints(n))
+        assert m.reserve(n)[0] == 0
+        p = rng.permutation(seqs)
+        p[rng.random(seqs) < 0.3] = -1
+        c.fork(ints(p.tolist()))
+        m.fork(p.tolist())
+        assert_tables(c, m)
+    n = [min(k, 70) for k in m.lens]
+    c.compact(ints([list(range(70))] * seqs), ints(n))
+    m.compact(n, 70)
+    assert_tables(c, m)
+    c.reserve(ints([seq_pages * 64 - k for k in m.lens]))      # more than there is, unless the slots hold it all
+    m.reserve([seq_pages * 64 - k for k in m.lens])
+    assert_tables(c, m)
+    assert c.status() in (0, R.NO_PAGES)
 
 
 def test_shared_last_page_is_copied_before_it_grows():
@@ -523,10 +573,11 @@ def test_bad_indexes_are_reported_and_harmless():
             assert not k[1].any() and not v[1].any() and not k[3].any() and k[0].any()
     assert c.lens.cpu().tolist() == [0, 256, 5] and c.table.cpu().tolist() == [[-1] * 4, [4, 5, 6, 7], [-1] * 4]
     for bad in ([0, 3, 1, 4], [0, 2, 9, 9], [-1, 2, 3, 4]):
-        c.status_word.zero_()
-        c.write(0, q[:, :2].contiguous(), q[:, 2:4].contiguous(), ints(bad))
-        assert c.status() & R.BAD_INDEX
-        c.attn(0, q, ints(bad))
+        for call in (lambda s: c.write(0, q[:, :2].contiguous(), q[:, 2:4].contiguous(), s), lambda s: c.attn(0, q, s),
+                     lambda s: c.read(0, s, 4)):
+            c.status_word.zero_()
+            call(ints(bad))
+            assert c.status() & R.BAD_INDEX
 
 
 # ---------------------------------------------------- graphs, other streams --
