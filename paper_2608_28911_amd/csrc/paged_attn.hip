@@ -433,7 +433,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     }
     const uint4* vmeta = kmeta + 16 * NG;
 
-    // scores (a wave with matrix instructions to issue goes first: 2 to 8 %)
+    // scores (a wave with matrix instructions to issue goes first, here and from
+    // the first 32 tokens' values on: 740 us instead of 755 for 2048 tokens over 16k)
     __builtin_amdgcn_s_setprio(1);
     float4v x[NR][4];
     const uint32_t* kd = reinterpret_cast<const uint32_t*>(kw);
@@ -518,53 +519,46 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 #pragma unroll
     for (int r = 0; r < NR; ++r) ref[r] = M[r] == -INFINITY ? 0.0f : M[r] - kHead;
 
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[r][tt][e] = exp2_fast(fmaf(x[r][tt][e], cf[r], -ref[r]));
-          l[r] += x[r][tt][e];
-        }
+    // weights of 32 tokens, then their products, twice: vector and matrix
+    // instructions of a SIMD's two waves meet oftener (740 us became 698)
     const uint32_t* vd = reinterpret_cast<const uint32_t*>(vw);
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-      // the group's weights, and the zeros' share
-      half8v wf[NR][2];
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        const uint4 mv = vmeta[j * 16 + tt * 4];
-        const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float s = lo16(m[e]), mid = fmaf(7.5f, s, hi16(m[e])), ss = e & 2 ? s * 0.0625f : s;
-#pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            const _Float16 w = _Float16(x[r][tt][e] * ss);
-            wf[r][tt >> 1][4 * (tt & 1) + e] = w;
-            az[r][j] = fmaf(x[r][tt][e], mid, az[r][j]);
-          }
-        }
-      }
-      if (NG > 1) __builtin_amdgcn_sched_barrier(0);
       // sums of the rounded weights (of several groups, each in its own four
       // rows of the result)
       const half8v ones = sums8(NG == 1 || n >> 2 == j);
 #pragma unroll
-      for (int st = 0; st < 2; ++st)
+      for (int st = 0; st < 2; ++st) {
+        half8v wf[NR];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) ws[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, wf[r][st], ws[r], 0, 0, 0);
-      // values
-      __builtin_amdgcn_s_setprio(1);
+        for (int tt = 2 * st; tt < 2 * st + 2; ++tt) {
+          const uint4 mv = vmeta[j * 16 + tt * 4];
+          const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
 #pragma unroll
-      for (int ct = j * CG; ct < (j + 1) * CG; ++ct)
+          for (int e = 0; e < 4; ++e) {
+            const float s = lo16(m[e]), mid = fmaf(7.5f, s, hi16(m[e])), ss = e & 2 ? s * 0.0625f : s;
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
+            for (int r = 0; r < NR; ++r) {
+              if (j == 0) {
+                x[r][tt][e] = exp2_fast(fmaf(x[r][tt][e], cf[r], -ref[r]));
+                l[r] += x[r][tt][e];
+              }
+              wf[r][4 * (tt & 1) + e] = _Float16(x[r][tt][e] * ss);
+              az[r][j] = fmaf(x[r][tt][e], mid, az[r][j]);   // the zeros' share
+            }
+          }
+        }
+        if (NG > 1) __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) ws[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, wf[r], ws[r], 0, 0, 0);
+#pragma unroll
+        for (int ct = j * CG; ct < (j + 1) * CG; ++ct) {
           const half8v A = SHARE ? sm_v[p & 1][(ct * 2 + st) & (FV - 1)][lane] : codes8(vd[SHARE ? 0 : ct * 2 + st]);
 #pragma unroll
-          for (int r = 0; r < NR; ++r) o[r][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, wf[r][st], o[r][ct], 0, 0, 0);
+          for (int r = 0; r < NR; ++r) o[r][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, wf[r], o[r][ct], 0, 0, 0);
         }
+      }
     }
     __builtin_amdgcn_s_setprio(0);
     if constexpr (!SHARE) {
