@@ -5,7 +5,10 @@
 // One pass over a row: each lane keeps its running maximum m and, relative to
 // it, S = sum e^(x-m) and T = sum e^(x-m) (x-m) in fp32 (the entropy is
 // ln S - T/S); the lanes' states join at the end.  Memory-bound: a logit is
-// read once.  The likeliest tokens are kept sorted across the lanes of a wave,
+// read once (4096 rows of 128000 fp16 logits 185 us, 5.7 TB/s; 4 rows, 15 workgroups
+// each, with five alternatives 9.8 us and 4.4 for their merge, which latency
+// bounds).  A workgroup of 4 waves takes a row, or a share of one where there are
+// few.  The likeliest tokens are kept sorted across the lanes of a wave,
 // as 64-bit keys of the logit's order and the complemented index; a vector of
 // logits is looked at again only if its maximum beats the wave's last kept one,
 // which happens k ln(n/k) times for n logits in random order.
