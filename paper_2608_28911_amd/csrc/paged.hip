@@ -7,7 +7,7 @@
 // times, 16 slots of 33 pages: reserve 5.3 us, the copies of 10 shared pages of
 // 557 KB 4.0, fork 3.0 + 3.1; a launch alone is 2.2).  The calls on rows are
 // memory-bound from some thousand rows on (8 kv heads, D = G = 128, fp16): 76000
-// rows are written in 95 us (4.1 TB/s of rows in and records out) and read in 75
+// rows are written in 88 us (4.5 TB/s of rows in and records out) and read in 75
 // (5.2 TB/s); 15600 of 62000 tokens of 4 layers move in 77 us; one row of each of
 // 16 sequences is written in 3.5 us.
 #include <hip/hip_fp16.h>
@@ -514,7 +514,7 @@ __device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uin
 // V, or one of them (a.parts == 2, where there are few pages).
 // Four lanes own a token row, D/4 channels each (with 16 lanes a row, loads
 // coalesce better, but a group's parameters, two divisions, are worked out in
-// four times as many lanes: 140 us instead of 96 for 76000 rows of 8 heads);
+// four times as many lanes: 140 us instead of 110 for 76000 rows of 8 heads);
 // the codes go to LDS as bytes and come out as the words of the record's
 // layout.  A page that the rows fill only in part keeps its other rows: K
 // words belong to one row, V words hold 8 tokens and are merged with what is
@@ -774,7 +774,7 @@ static void write_of(const PagedWriteArgs& a, dim3 grid, hipStream_t s) {
 
 int launch_paged_write(PagedWriteArgs a, hipStream_t s) {
   // K and V in workgroups of their own where there are few: 2048 rows of 8
-  // heads 7.8 us, 9.1 together; 76000 rows 110 us, 95 together
+  // heads 6.4 us, 7.3 together; 16384 rows 26.4, 24.5; 76000 rows 104, 87.5
   const int64_t bound = touched_bound(a.r);
   a.parts = bound * a.c.n_kv_heads * a.layers < 2048 ? 2 : 1;
   const dim3 grid(unsigned(bound), unsigned(a.c.n_kv_heads), unsigned(a.parts * a.layers));

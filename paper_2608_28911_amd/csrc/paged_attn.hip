@@ -22,8 +22,8 @@
 // What bounds it (8 kv heads of 128 channels, 4 query heads each, one group a
 // row): a batch of long contexts memory, 16 sequences of 8 to 16k tokens 49 us at
 // 4.5 TB/s; one sequence latency, 2k tokens 9.6 us, 32k 14.5 (2.4 of launch, 2.5 to
-// the first record, 2.7 to join the splits); chunks vector instructions, 63 % of
-// whose issue slots are taken, beside 33 % of the matrix cores': 2048 tokens over
+// the first record, 2.7 to join the splits); chunks vector instructions, 66 % of
+// whose issue slots are taken, beside 34 % of the matrix cores': 2048 tokens over
 // 16k 698 us, 836 TFLOP/s.
 //
 // Softmax: one pass with a running reference M per row.  It includes the
