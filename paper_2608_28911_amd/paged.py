@@ -53,6 +53,7 @@ def _setup():
 
 def _enqueue(index, f, what, *args):
     """f(*args, stream) with device `index` current, on its current stream."""
+    _need(index >= 0, "%s: the buffers must be on a GPU", what)
     if _torch is None:
         _setup()
     if _device() == index:

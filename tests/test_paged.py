@@ -154,6 +154,21 @@ def test_binding_checks_what_it_is_given(bound):
     assert a[1] == 0 and a[4:8] == (0, 0, 1024, 128) and a[9:11] == (2, 5)
 
 
+def test_a_cache_in_host_memory_is_refused(monkeypatch):
+    """Its addresses must not reach a kernel."""
+    import torch
+    import paper_2608_28911_amd as P
+    from paper_2608_28911_amd import paged
+    rec = Recorder()
+    sizes = P.paged_sizes(config(n_pages=8, seq_pages=4))
+    monkeypatch.setattr(paged, "paged_sizes", lambda cfg: sizes)
+    monkeypatch.setattr(paged, "lib", lambda: rec)
+    for kw in ({"device": "cpu"}, {"device": "meta"}, {"pool": torch.empty(sizes.pool_bytes, dtype=torch.uint8)}):
+        with pytest.raises(ValueError):
+            P.PagedKV4(config(n_pages=8, seq_pages=4), **kw)
+        assert not rec.calls, kw
+
+
 def test_binding_of_logprobs_checks_what_it_is_given():
     import torch
     import paper_2608_28911_amd as P
