@@ -21,8 +21,9 @@
 //
 // What bounds it (8 kv heads of 128 channels, 4 query heads each, one group a
 // row): a batch of long contexts memory, 16 sequences of 8 to 16k tokens 49 us at
-// 4.5 TB/s; one sequence latency, 2k tokens 9.6 us, 32k 14.5 (2.4 of launch, 2.5 to
-// the first record, 2.7 to join the splits); chunks vector instructions, 66 % of
+// 4.5 TB/s; one sequence latency, 2k tokens 9.6 us, 32k 14.5 (by builds that leave
+// parts out, when it took 15 to 16: 2.5 with the launch until a workgroup knows its
+// tile, 5 for its pages, 2.7 to join the splits); chunks vector instructions, 66 % of
 // whose issue slots are taken, beside 34 % of the matrix cores': 2048 tokens over
 // 16k 698 us, 836 TFLOP/s.
 //
@@ -119,7 +120,7 @@ struct Tile {
 // The pages of a call are shared out by what the sequences really hold: the
 // call's tiles times pages over the workgroups wanted for a kv head (a.target)
 // make a share (`chunk`), which grows until as many workgroups do: one more
-// than fit the chip at once costs as much as a whole round (4 x 32k tokens, 8
+// than fit the chip at once costs as much as filling it again (4 x 32k tokens, 8
 // waves a workgroup: 27 us instead of 41).  A sequence is split where it holds
 // more than a share and kWhole pages, into kMostSplits at most: joining costs
 // 2 us (500 tokens 7.0 us whole, 8.8 in two) and 0.05 more for each split.
@@ -441,7 +442,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     const uint4* vmeta = kmeta + 16 * NG;
 
     // scores (a wave with matrix instructions to issue goes first, here and from
-    // the first 32 tokens' values on: 740 us instead of 755 for 2048 tokens over 16k)
+    // the first 32 tokens' values on: without the latter 722 us instead of 698 for
+    // 2048 tokens over 16k)
     __builtin_amdgcn_s_setprio(1);
     float4v x[NR][4];
     const uint32_t* kd = reinterpret_cast<const uint32_t*>(kw);
@@ -782,7 +784,7 @@ int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// counters, and kSlots partials of the widest tile
+// counters, and 2 kSlots partials of the widest tile for each kv head
 size_t paged_attn_workspace(int d) { return size_t(kCounterWords + 2 * kSlots * 32 * (d + 4)) * 4; }
 
 int launch_paged_attn(PagedAttnArgs a, size_t ws_bytes, hipStream_t s) {
