@@ -370,7 +370,9 @@ int semkv_paged_init(semkv_paged* c, const semkv_paged_config* cfg, void* pool, 
  * [max_seqs][seq_pages], entry c of a row used where 64c < its length.
  * Counts and free pages follow.  A length outside [0, 64 seq_pages] is
  * clamped, an entry outside [0, n_pages) becomes -1 (SEMKV_STATUS_BAD_INDEX):
- * its tokens are not cached. */
+ * its tokens are not cached.  lens and table may be the cache's own (shorter
+ * lengths over its own table drop its sequences' last tokens); arguments that
+ * overlap the state otherwise are refused. */
 int semkv_paged_assign(semkv_paged* c, const int32_t* lens, const int32_t* table, hipStream_t stream);
 
 /* Room for n_new[s] more tokens of every sequence s (device int32
@@ -381,7 +383,9 @@ int semkv_paged_assign(semkv_paged* c, const int32_t* lens, const int32_t* table
  * If the free pages or seq_pages do not suffice, nothing changes,
  * SEMKV_STATUS_NO_PAGES is set, and semkv_paged_write stores nothing until a
  * semkv_paged_reserve succeeds.  A negative count is taken as 0
- * (SEMKV_STATUS_BAD_INDEX). */
+ * (SEMKV_STATUS_BAD_INDEX).  The arguments of this call and of the next two may
+ * be the cache's own lengths or table; ones that reach behind those in the
+ * state are refused. */
 int semkv_paged_reserve(semkv_paged* c, const int32_t* n_new, hipStream_t stream);
 
 /* Every slot s takes over the contents that slot parent[s] had before the call

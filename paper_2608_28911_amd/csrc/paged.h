@@ -124,7 +124,7 @@ __device__ inline int find_tile(int n_seqs, int flat, int lane, F tiles, int& ti
   return -1;
 }
 
-int launch_paged_clear(const PagedView& c, hipStream_t s);
+int launch_paged_clear(const PagedView& c, int tables, hipStream_t s);
 int launch_paged_assign(const PagedView& c, const int32_t* lens, const int32_t* table, hipStream_t s);
 int launch_paged_reserve(const PagedView& c, const int32_t* n_new, hipStream_t s);
 int launch_paged_fork(const PagedView& c, const int32_t* parent, hipStream_t s);

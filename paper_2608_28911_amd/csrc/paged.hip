@@ -83,14 +83,15 @@ __device__ inline void release(const PagedView& c, int p) {
   if (atomicSub(c.refs + p, 1) == 1) atomicOr(c.free + (p >> 5), 1u << (p & 31));
 }
 
-__global__ __launch_bounds__(256) void paged_clear_kernel(PagedView c) {
+// Every page free; `tables`: every sequence empty too.
+__global__ __launch_bounds__(256) void paged_clear_kernel(PagedView c, int tables) {
   const int64_t i0 = int64_t(blockIdx.x) * 256 + threadIdx.x, step = int64_t(gridDim.x) * 256;
-  for (int64_t i = i0; i < int64_t(c.max_seqs) * c.seq_pages; i += step) c.table[i] = -1;
-  for (int64_t i = i0; i < c.n_pages; i += step) c.refs[i] = 0;
-  for (int64_t i = i0; i < c.max_seqs; i += step) {
-    c.lens[i] = 0;
-    c.cow[2 * i] = -1;
+  if (tables) {
+    for (int64_t i = i0; i < int64_t(c.max_seqs) * c.seq_pages; i += step) c.table[i] = -1;
+    for (int64_t i = i0; i < c.max_seqs; i += step) c.lens[i] = 0;
   }
+  for (int64_t i = i0; i < c.n_pages; i += step) c.refs[i] = 0;
+  for (int64_t i = i0; i < c.max_seqs; i += step) c.cow[2 * i] = -1;
   const int words = (c.n_pages + 31) / 32;
   for (int64_t i = i0; i < words; i += step) {
     const int left = c.n_pages - int(32 * i);
@@ -99,8 +100,10 @@ __global__ __launch_bounds__(256) void paged_clear_kernel(PagedView c) {
   if (i0 == 0) *c.stalled = 0;
 }
 
-// The caller's tables over empty ones (paged_clear_kernel): entries in use are
-// copied and counted.
+// The caller's tables, where every page is free (paged_clear_kernel): entries
+// in use are copied and counted.  `lens` and `table` may be the cache's own: a
+// thread reads the one entry that it writes, and a length that is the cache's
+// own is written back as it was.
 __global__ __launch_bounds__(256) void paged_assign_kernel(PagedView c, const int32_t* lens, const int32_t* table) {
   const int s = blockIdx.y, col = blockIdx.x * 256 + threadIdx.x;
   const int given = lens[s], most = kPage * c.seq_pages;
@@ -109,14 +112,16 @@ __global__ __launch_bounds__(256) void paged_assign_kernel(PagedView c, const in
     c.lens[s] = len;
     if (len != given) atomicOr(c.status, kBad);
   }
-  if (col >= div_up(len, kPage)) return;
+  if (col >= c.seq_pages) return;
   const int64_t at = int64_t(s) * c.seq_pages + col;
-  const int p = table[at];
-  if (p < 0 || p >= c.n_pages) {
-    atomicOr(c.status, kBad);
+  const bool used = col < div_up(len, kPage);
+  const int p = used ? table[at] : -1;
+  const bool there = p >= 0 && p < c.n_pages;
+  c.table[at] = there ? p : -1;
+  if (!there) {
+    if (used) atomicOr(c.status, kBad);
     return;
   }
-  c.table[at] = p;
   hold(c, p);
   atomicAnd(c.free + (p >> 5), ~(1u << (p & 31)));
 }
@@ -725,16 +730,16 @@ inline dim3 table_grid(const PagedView& c) { return dim3(unsigned((c.seq_pages +
 
 }  // namespace
 
-int launch_paged_clear(const PagedView& c, hipStream_t s) {   // no sequence holds a token
-  int64_t n = int64_t(c.max_seqs) * c.seq_pages;
+int launch_paged_clear(const PagedView& c, int tables, hipStream_t s) {
+  int64_t n = tables ? int64_t(c.max_seqs) * c.seq_pages : c.max_seqs;
   if (n < c.n_pages) n = c.n_pages;
   const int64_t blocks = (n + 255) / 256;
-  hipLaunchKernelGGL(paged_clear_kernel, dim3(unsigned(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, c);
+  hipLaunchKernelGGL(paged_clear_kernel, dim3(unsigned(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, c, tables);
   return done();
 }
 
 int launch_paged_assign(const PagedView& c, const int32_t* lens, const int32_t* table, hipStream_t s) {
-  const int st = launch_paged_clear(c, s);
+  const int st = launch_paged_clear(c, 0, s);
   if (st) return st;
   hipLaunchKernelGGL(paged_assign_kernel, table_grid(c), dim3(256), 0, s, c, lens, table);
   return done();

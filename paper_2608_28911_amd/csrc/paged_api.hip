@@ -55,6 +55,19 @@ int rows_of(const semkv_paged* c, const int32_t* starts, int32_t n_seqs, int64_t
   return 0;
 }
 
+// Whether n words at p lie, in part at least, in words [word, end) of the state.
+bool inside(const semkv_paged* c, const int32_t* p, int64_t n, int64_t word, int64_t end) {
+  const uintptr_t a = uintptr_t(p), state = uintptr_t(c->state);
+  return n > 0 && a < state + 4 * end && a + 4 * n > state + 4 * word;
+}
+
+// An argument of reserve, fork or compact in what follows the tables, which
+// their kernels write while others of their workgroups still read arguments.
+// (Lengths and tables are written last: an argument may lie there.)
+bool scratched(const semkv_paged* c, const int32_t* p, int64_t n) {
+  return inside(c, p, n, c->sz.refs_word, int64_t(c->sz.state_bytes / 4));
+}
+
 constexpr int64_t kMaxRows = (int64_t(1) << 24) - 1;
 
 bool layer_ok(const semkv_paged* c, int32_t layer, int32_t least) { return layer >= least && layer < c->cfg.n_layers; }
@@ -103,28 +116,34 @@ int semkv_paged_init(semkv_paged* c, const semkv_paged_config* cfg, void* pool, 
   c->pool = static_cast<uint8_t*>(pool);
   c->state = state;
   c->status = status;
-  return launch_paged_clear(view(c), stream);
+  return launch_paged_clear(view(c), 1, stream);
 }
 
 int semkv_paged_assign(semkv_paged* c, const int32_t* lens, const int32_t* table, hipStream_t stream) {
   if (!c || !lens || !table) return SEMKV_EINVAL;
   if ((uintptr_t(lens) | uintptr_t(table)) & 3) return SEMKV_EINVAL;
-  return launch_paged_assign(view(c), lens, table, stream);
+  const PagedView v = view(c);
+  const int64_t end = int64_t(c->sz.state_bytes / 4);
+  if (lens != v.lens && inside(c, lens, v.max_seqs, 0, end)) return SEMKV_EINVAL;
+  if (table != v.table && inside(c, table, int64_t(v.max_seqs) * v.seq_pages, 0, end)) return SEMKV_EINVAL;
+  return launch_paged_assign(v, lens, table, stream);
 }
 
 int semkv_paged_reserve(semkv_paged* c, const int32_t* n_new, hipStream_t stream) {
-  if (!c || !n_new || (uintptr_t(n_new) & 3)) return SEMKV_EINVAL;
+  if (!c || !n_new || (uintptr_t(n_new) & 3) || scratched(c, n_new, c->cfg.max_seqs)) return SEMKV_EINVAL;
   return launch_paged_reserve(view(c), n_new, stream);
 }
 
 int semkv_paged_fork(semkv_paged* c, const int32_t* parent, hipStream_t stream) {
-  if (!c || !parent || (uintptr_t(parent) & 3)) return SEMKV_EINVAL;
+  if (!c || !parent || (uintptr_t(parent) & 3) || scratched(c, parent, c->cfg.max_seqs)) return SEMKV_EINVAL;
   return launch_paged_fork(view(c), parent, stream);
 }
 
 int semkv_paged_compact(semkv_paged* c, const int32_t* keep, int64_t ld_keep, const int32_t* n_keep, hipStream_t stream) {
   if (!c || !n_keep || ld_keep < 0 || (ld_keep > 0 && !keep)) return SEMKV_EINVAL;
   if ((uintptr_t(keep) | uintptr_t(n_keep)) & 3) return SEMKV_EINVAL;
+  const int64_t ld = ld_keep < (int64_t(1) << 40) ? ld_keep : int64_t(1) << 40;
+  if (scratched(c, keep, ld * c->cfg.max_seqs) || scratched(c, n_keep, c->cfg.max_seqs)) return SEMKV_EINVAL;
   return launch_paged_compact(view(c), keep, ld_keep, n_keep, stream);
 }
 

@@ -130,7 +130,8 @@ class PagedKV4:
 
     # -- pages -------------------------------------------------------------
     def assign(self, lens, table):
-        """Take over lengths [max_seqs] and page tables [max_seqs, seq_pages], int32."""
+        """Take over lengths [max_seqs] and page tables [max_seqs, seq_pages], int32; either may be the cache's own
+        (shorter lengths over self.table drop the sequences' last tokens)."""
         _enqueue(self._at, self._lib.semkv_paged_assign, "semkv_paged_assign", self._ref,
                  self._ints(lens, "lens", self._seqs), self._ints(table, "table", self._seqs, self._width))
 

@@ -1,0 +1,23 @@
+"""Refusals of the paged cache's calls over buffers that overlap: no GPU."""
+import ctypes
+
+from tests.test_paged import abi, cache  # noqa: F401
+
+
+def test_arguments_inside_the_state_are_refused(abi, cache):  # noqa: F811
+    """The calls write what follows the tables in the state, so their arguments
+    must not lie there; assign writes the tables too, and takes them in place
+    only."""
+    f, c, sz = abi.lib(), ctypes.byref(cache), cache.sz
+    at = lambda word: ctypes.c_void_p(cache.state + 4 * word)  # noqa: E731
+    far, end = ctypes.c_void_p(0x100000), sz.state_bytes // 4
+    for w in (0, 60, sz.lens_word + 1, sz.lens_word - 1, sz.table_word, sz.table_word - 1, sz.refs_word, sz.scratch_word, end - 1):
+        assert f.semkv_paged_assign(c, at(w), far, None) == -1, w
+    for w in (-1, 0, sz.lens_word, sz.table_word - 1, sz.table_word + 50, sz.refs_word, end - 1):
+        assert f.semkv_paged_assign(c, far, at(w), None) == -1, w
+    for w in (sz.refs_word - 1, sz.refs_word, sz.free_word, sz.scratch_word, end - 1):
+        assert f.semkv_paged_reserve(c, at(w), None) == -1, w
+        assert f.semkv_paged_fork(c, at(w), None) == -1, w
+        assert f.semkv_paged_compact(c, far, 8, at(w), None) == -1, w
+        assert f.semkv_paged_compact(c, at(w), 8, far, None) == -1, w
+    assert f.semkv_paged_compact(c, at(sz.refs_word - 31), 8, far, None) == -1     # its last entry lies there
