@@ -411,9 +411,11 @@ int semkv_paged_compact(semkv_paged* c, const int32_t* keep, int64_t ld_keep, co
  * sequence s are rows starts[s] .. starts[s+1]-1 (device int32 [n_seqs+1],
  * ascending), its last starts[s+1]-starts[s] tokens in order; n_rows bounds
  * them all (at most 2^28).  Rows from starts[n_seqs] on (a padded batch) are neither read nor
- * written.  Starts that descend or pass n_rows set SEMKV_STATUS_BAD_INDEX, and
- * the sequence has no row; so do, in semkv_paged_write and _read, more rows
- * than the sequence has tokens, whose first then have no place in the cache.
+ * written.  Starts that descend or pass n_rows set SEMKV_STATUS_BAD_INDEX: the
+ * sequence has no row, nor has one whose rows would begin before those of an
+ * earlier one end, so that no row is two sequences'.  More rows than the
+ * sequence has tokens set it too in semkv_paged_write and _read: the first then
+ * have no place in the cache.
  *
  * Quantize rows of K and V into the pages: element (row t, kv head h, channel
  * j) at t*sT + h*sH + j (+ l*sL with layer == -1, every layer), dtype

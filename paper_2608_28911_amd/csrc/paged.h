@@ -85,12 +85,34 @@ struct TokenArgs {
   float* ws;
 };
 
-// A sequence's share of a call's rows; count 0 where its starts are unusable.
+// A sequence's share of a call's rows; count 0 where it has none.
 struct SeqRows { int32_t first, count; };
-__device__ inline SeqRows seq_rows(const PagedRows& r, int s) {
+
+// The rows of sequences s0 .. s0+63, one to a lane of the wave.  A sequence has
+// none where its starts descend or pass the rows there are, nor where they begin
+// before an earlier sequence's rows end: no row is two sequences', and no call
+// has more rows in all than the host counted for its grid (a tile of which only
+// some workgroups existed would leave its counter behind).  reached: where the
+// rows of the sequences before s0 end; moved past these where more follow.  len:
+// the sequence's tokens.  All three loads are under way before the first is
+// looked at (a row of each of 16 sequences is read in 4.1 us, with loads behind
+// conditions in 4.5).
+__device__ inline SeqRows lane_rows(const PagedView& c, const PagedRows& r, int s0, int lane, int& reached, int& len) {
+  const bool mine = s0 + lane < r.n_seqs;
+  const int s = min(s0 + lane, r.n_seqs - 1), rows = int(r.n_rows);
   const int32_t a = r.starts[s], b = r.starts[s + 1];
-  if (a < 0 || b <= a || b > r.n_rows) return {a, 0};
-  return {a, b - a};
+  len = c.lens[s];
+  bool ok = mine && a >= 0 && b > a && b <= rows;
+  int end = b;                          // of this and the earlier sequences' rows, where starts ascend
+  if (__builtin_expect(__any(a < reached || b < a || b > rows), 0)) {
+    end = ok ? b : 0;
+#pragma unroll 1
+    for (int d = 1; d < 64; d <<= 1) end = max(end, __shfl_up(end, d));
+    const int before = __shfl_up(end, 1);
+    ok = ok && a >= max(reached, lane ? before : 0);
+  }
+  if (s0 + 64 < r.n_seqs) reached = max(reached, __builtin_amdgcn_readlane(end, 63));
+  return {a, ok ? b - a : 0};
 }
 
 // Starts that descend, or pass the rows there are.
@@ -99,13 +121,17 @@ __device__ inline bool starts_bad(const PagedRows& r, int s) {
   return a < 0 || b < a || b > r.n_rows;
 }
 
-// Which sequence's tile a flat index names, where sequence s has tiles(s) of
-// them: the whole wave counts 64 sequences at a time.  -1 past the last.
+// Which sequence's tile a flat index names, where a sequence of `len` tokens
+// and `count` rows has tiles(len, count) of them; and its rows and tokens.  The
+// whole wave counts 64 sequences at a time.  -1 past the last.
 template <class F>
-__device__ inline int find_tile(int n_seqs, int flat, int lane, F tiles, int& tile) {
-  int before = 0;
-  for (int s0 = 0; s0 < n_seqs; s0 += 64) {
-    int n = s0 + lane < n_seqs ? tiles(s0 + lane) : 0, incl = n;
+__device__ inline int find_tile(const PagedView& c, const PagedRows& r, int flat, int lane, F tiles, int& tile, SeqRows& rows,
+                                int& len) {
+  int before = 0, reached = 0;
+  for (int s0 = 0; s0 < r.n_seqs; s0 += 64) {
+    int own;
+    const SeqRows mine = lane_rows(c, r, s0, lane, reached, own);
+    int n = tiles(own, mine.count), incl = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int up = __shfl_up(incl, d);
@@ -116,6 +142,8 @@ __device__ inline int find_tile(int n_seqs, int flat, int lane, F tiles, int& ti
       const int l = __ffsll((unsigned long long)above) - 1;
       const int start = before + __shfl(incl - n, l);
       tile = flat - start;
+      rows = {__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.count, l)};
+      len = __builtin_amdgcn_readlane(own, l);
       return __builtin_amdgcn_readfirstlane(s0 + l);
     }
     before += __shfl(incl, 63);

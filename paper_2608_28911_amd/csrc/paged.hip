@@ -373,14 +373,14 @@ __device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int
   PageWork k;
   int tile;
   const int lane = threadIdx.x & 63;
-  k.seq = find_tile(r.n_seqs, flat, lane,
-                    [&](int s) { return pages_touched(c.lens[s], seq_rows(r, s).count); }, tile);
+  SeqRows m = {0, 0};
+  int len = 0;
+  k.seq = find_tile(c, r, flat, lane, [](int n, int count) { return pages_touched(n, count); }, tile, m, len);
   k.page = -1;
   k.lo = k.hi = 0;
   k.row0 = 0;
   if (k.seq < 0) return k;
-  const SeqRows m = seq_rows(r, k.seq);
-  const int len = c.lens[k.seq], first = max(len - m.count, 0);
+  const int first = max(len - m.count, 0);
   const int col = first / kPage + tile;
   k.page = c.table[int64_t(k.seq) * c.seq_pages + col];
   k.lo = max(first - col * kPage, 0);
@@ -659,13 +659,16 @@ __device__ inline void store8(void* p, int64_t at, const float (&v)[8]) {
 }
 
 // Rows that would precede their sequence's first token: zeros.  Rare, so a
-// thread takes a whole sequence's.
+// thread takes a whole sequence's, and one wave all of them.
 template <int D, int DT>
 __device__ inline void early_rows(const PagedReadArgs& a, int head) {
+  if (threadIdx.x >= 64) return;
   const float zeros[8] = {};
-  for (int s = threadIdx.x; s < a.r.n_seqs; s += blockDim.x) {
-    const SeqRows m = seq_rows(a.r, s);
-    for (int i = 0; i < m.count - a.c.lens[s]; ++i) {
+  int reached = 0;
+  for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
+    int len;
+    const SeqRows m = lane_rows(a.c, a.r, s0, threadIdx.x, reached, len);
+    for (int i = 0; i < m.count - len; ++i) {
       const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + m.first + i) * a.c.n_kv_heads + head) * D;
       for (int j = 0; j < D; j += 8) {
         store8<DT>(a.K, at + j, zeros);

@@ -135,22 +135,21 @@ __device__ inline int splits_of(int pages, int chunk) {
 template <int ROWS>
 __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
   struct Share { int first, count, len, tiles, pages; };
-  auto share = [&](int s) {
-    Share k = {0, 0, 0, 0, 0};
-    if (s < a.r.n_seqs) {
-      const SeqRows m = seq_rows(a.r, s);
-      k.first = m.first;
-      k.count = m.count;
-      k.len = a.c.lens[s];
-      k.tiles = (m.count * a.gqa + ROWS - 1) / ROWS;
-      k.pages = (k.len + kPage - 1) / kPage;
-    }
+  auto share = [&](int s0, int& reached) {
+    Share k;
+    const SeqRows m = lane_rows(a.c, a.r, s0, lane, reached, k.len);
+    k.first = m.first;
+    k.count = m.count;
+    k.tiles = (m.count * a.gqa + ROWS - 1) / ROWS;
+    k.pages = (k.len + kPage - 1) / kPage;
     return k;
   };
-  Share mine = share(lane);
+  int reached = 0;
+  Share mine = share(0, reached);
+  const int reached64 = reached;
   int64_t work = int64_t(mine.tiles) * mine.pages;
   for (int s0 = 64; s0 < a.r.n_seqs; s0 += 64) {
-    const Share k = share(s0 + lane);
+    const Share k = share(s0, reached);
     work += int64_t(k.tiles) * k.pages;
   }
   const int width = min(a.r.n_seqs, 64);           // lanes that hold a sequence
@@ -175,8 +174,9 @@ __device__ inline Tile tile_of(const PagedAttnArgs& a, int flat, int lane) {
   Tile k;
   k.seq = -1;
   int before = 0, parts = 0, sp = 1;
+  reached = reached64;
   for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
-    if (s0) mine = share(s0 + lane);
+    if (s0) mine = share(s0, reached);
     const int splits = splits_of(mine.pages, chunk);
     const int n = mine.tiles * splits, held = splits > 1 ? n : 0;
     int incl = n, pincl = held;

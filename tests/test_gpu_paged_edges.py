@@ -1,11 +1,12 @@
 """Calls of the paged 4-bit cache at the edges of what its header allows:
-arguments that are the cache's own buffers.  Against the plain model of
-tests/pagedref.py."""
+arguments that are the cache's own buffers, malformed starts.  Against the
+plain model of tests/pagedref.py; attention's tolerance is the one worked out
+in tests/test_gpu_paged.py."""
 import numpy as np
 import pytest
 
 from tests import pagedref as R
-from tests.test_gpu_paged import assert_tables, fill, ints, make, starts_of
+from tests.test_gpu_paged import assert_tables, check_attn, fill, ints, make, rows, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,101 @@ def test_own_lengths_as_counts():
     m.fork([3, 1, 0, 2])
     assert_tables(c, m)
     assert c.status() == 0
+
+
+# --------------------------------------------------------- malformed starts --
+
+def accepted(starts, n_rows):
+    """First row and count of every sequence, by the header's words."""
+    out, reached = [], 0
+    for a, b in zip(starts, starts[1:]):
+        fine = 0 <= a < b <= n_rows
+        out.append((a, b - a) if fine and a >= reached else (a, 0))
+        reached = max(reached, b) if fine else reached
+    return out
+
+
+def check_accepted(c, lens, starts, q, out, lse):
+    """check_attn over the rows that sequences have; the others are as they were."""
+    import torch
+    acc = accepted(starts, q.shape[0])
+    at = [t for a, m in acc for t in range(a, a + m)]
+    if at:
+        check_attn(c, lens, [m for _, m in acc], q[at], out[at], lse[at], c.cfg.head_dim ** -0.5,
+                   only=lambda t, h: (t + h) % 11 == 0)
+    rest = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert torch.all(out[rest] == 7.0) and torch.all(lse[rest] == 7.0)
+
+
+def test_attn_counters_after_malformed_starts():
+    """Starts that would give two long sequences the same rows ask for more
+    workgroups than there are: the workspace is whole afterwards, and the next
+    call's results are those over a fresh one."""
+    import torch
+    rng = np.random.default_rng(60)
+    lens = [3000, 3000, 10, 64, 20000]
+    c = make(h=8, hq=32, n_pages=420, seqs=5, seq_pages=320)
+    fill(c, lens, rng)
+    q = rows(rng, (64, 32, 128), torch.float16) * 0.3
+    starts = [0, 64, 0, 64, 0, 64]
+    out, lse = torch.full_like(q, 7.0), torch.full((64, 32), 7.0, device="cuda")
+    c.attn(0, q, ints(starts), out=out, lse=lse)
+    check_accepted(c, lens, starts, q, out, lse)
+    assert c.status() == R.BAD_INDEX
+    assert not c.ws[:2 * 512 * 64].view(torch.int32).any()     # the counters
+    c.status_word.zero_()
+    good = starts_of([10, 10, 10, 10, 24])
+    first = c.attn(0, q, good, with_lse=True)
+    second = c.attn(0, q, good, with_lse=True, workspace=torch.zeros_like(c.ws))
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    check_attn(c, lens, [10, 10, 10, 10, 24], q, *first, 128 ** -0.5, only=lambda t, h: (t + h) % 11 == 0)
+    assert c.status() == 0
+
+
+@pytest.mark.parametrize("seqs", [3, 64, 130])
+def test_rows_of_malformed_starts(seqs):
+    """Starts that descend, pass the rows or reuse them, more sequences than a
+    wave has lanes among them: write, read and attention take exactly the rows
+    that the header gives a sequence, and leave the others alone."""
+    import torch
+    rng = np.random.default_rng(61 + seqs)
+    lens = [int(x) for x in rng.integers(1, 130, seqs)]
+    lens[seqs // 2] = 900
+    c = make(h=1, hq=4, d=64, g=32, n_pages=500, seqs=seqs, seq_pages=16)
+    fill(c, lens, rng)
+    n, table = 150, c.table.cpu().numpy()
+    for step in range(8):
+        starts = np.sort(rng.integers(0, n + 1, seqs + 1))
+        for _ in range(1 + seqs // 20):                  # some out of order, some out of range
+            starts[rng.integers(0, seqs + 1)] = rng.integers(-2, n + 3)
+        if step % 2:
+            starts[rng.integers(0, seqs):] = rng.integers(0, n // 2)
+        starts = starts.tolist()
+        acc = accepted(starts, n)
+        pool = c.pool.cpu().numpy().reshape(-1, c.sz.record_bytes)
+        K, V = rows(rng, (n, 1, 64), torch.float16), rows(rng, (n, 1, 64), torch.float16)
+        c.write(0, K, V, ints(starts))
+        for s, (a, m) in enumerate(acc):
+            for t in range(m):
+                pos = lens[s] - m + t
+                if pos < 0:
+                    continue
+                for kv, x in enumerate((K, V)):
+                    code, sc, z = R.quantize(x[a + t].cpu().float().numpy(), 32)
+                    R.store(pool[table[s, pos // 64]], pos % 64, kv, code[0], sc[0], z[0], 64, 32)
+        assert np.array_equal(c.pool.cpu().numpy().reshape(-1, c.sz.record_bytes), pool), step
+        back = [torch.full((n, 1, 64), 7.0, device="cuda") for _ in range(2)]
+        c.read(0, ints(starts), n, out=back)
+        want = [np.full((n, 64), 7.0, np.float32) for _ in range(2)]
+        for s, (a, m) in enumerate(acc):
+            for t in range(m):
+                pos = lens[s] - m + t
+                for w, v in zip(want, R.values(pool[table[s, max(pos, 0) // 64]], 64, 32)):
+                    w[a + t] = v[pos % 64] if pos >= 0 else 0.0
+        assert all(np.array_equal(b[:, 0].cpu().numpy(), w) for b, w in zip(back, want)), step
+        q = rows(rng, (n, 4, 64), torch.float16) * 0.3
+        out, lse = torch.full_like(q, 7.0), torch.full((n, 4), 7.0, device="cuda")
+        c.attn(0, q, ints(starts), out=out, lse=lse)
+        check_accepted(c, lens, starts, q, out, lse)
+        assert not c.ws[:2 * 512 * 64].view(torch.int32).any()
