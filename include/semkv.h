@@ -402,7 +402,7 @@ int semkv_paged_fork(semkv_paged* c, const int32_t* parent, hipStream_t stream);
  * its former pages are released.  n_keep[s] = -1 leaves s as it is.  If the
  * free pages do not suffice, nothing changes and SEMKV_STATUS_NO_PAGES is
  * set.  n_keep[s] outside [-1, min(ld_keep, 64 seq_pages)] is taken as -1, a
- * position outside the sequence gives a row of zeros
+ * position outside the sequence, or whose page is missing, gives a row of zeros
  * (SEMKV_STATUS_BAD_INDEX). */
 int semkv_paged_compact(semkv_paged* c, const int32_t* keep, int64_t ld_keep, const int32_t* n_keep,
                         hipStream_t stream);

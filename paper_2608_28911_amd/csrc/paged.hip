@@ -304,9 +304,9 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedView c, const int3
     int slot = 0;
     if (first + tid < n) {
       const int pos = keep[s * ld + first + tid];
-      if (pos >= 0 && pos < c.lens[s]) {
-        const int p = c.table[int64_t(s) * c.seq_pages + pos / kPage];
-        if (p >= 0) rec = paged_record_at(c, p, layer, head);
+      const int p = pos >= 0 && pos < c.lens[s] ? c.table[int64_t(s) * c.seq_pages + pos / kPage] : -1;
+      if (p >= 0) {
+        rec = paged_record_at(c, p, layer, head);
         slot = pos % kPage;
       } else if (layer == 0 && head == 0) {
         atomicOr(c.status, kBad);

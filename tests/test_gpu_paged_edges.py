@@ -1,7 +1,7 @@
 """Calls of the paged 4-bit cache at the edges of what its header allows:
-arguments that are the cache's own buffers, malformed starts.  Against the
-plain model of tests/pagedref.py; attention's tolerance is the one worked out
-in tests/test_gpu_paged.py."""
+arguments that are the cache's own buffers, malformed starts, missing pages.
+Against the plain model of tests/pagedref.py; attention's tolerance is the one
+worked out in tests/test_gpu_paged.py."""
 import numpy as np
 import pytest
 
@@ -169,3 +169,29 @@ def test_rows_of_malformed_starts(seqs):
         c.attn(0, q, ints(starts), out=out, lse=lse)
         check_accepted(c, lens, starts, q, out, lse)
         assert not c.ws[:2 * 512 * 64].view(torch.int32).any()
+
+
+# ------------------------------------------------------------ missing pages --
+
+def test_compact_reports_tokens_of_missing_pages():
+    """A kept token whose page is missing has no values: a row of zeros, as a
+    position outside the sequence gives, and reported like one."""
+    import torch
+    c = make(n_layers=2, n_pages=16, seqs=2, seq_pages=4)
+    fill(c, [150, 70], np.random.default_rng(52))
+    table = c.table.clone()
+    table[0, 1] = -1
+    c.assign(c.lens.clone(), table)
+    m = model_of(c)
+    keep = ints([[3, 64, 140], [0, 69, 0]])
+    before = c.read(-1, starts_of([150, 70]), 220)
+    c.status_word.zero_()
+    c.compact(keep, ints([3, 2]))
+    m.compact([3, 2], 3)
+    assert_tables(c, m)
+    assert c.status() == R.BAD_INDEX
+    for x, y in zip(before, c.read(-1, starts_of([3, 2]), 5)):
+        assert not y[:, 1].any() and torch.equal(y[:, [0, 2, 3, 4]], x[:, [3, 140, 150, 219]])
+    c.status_word.zero_()
+    c.compact(ints([[0, 2], [1, 0]]), ints([2, 1]))      # every page is there now
+    assert c.status() == 0
