@@ -42,13 +42,14 @@ _torch = None
 
 def _setup():
     """torch's functions that every call needs, looked up once: the current
-    device, and a device's current stream as an integer."""
+    device, and a device's current stream as an integer.  _torch says that they
+    are there, and is set last: another thread may be looking."""
     global _torch, _device, _stream_of
     import torch
-    _torch = torch
     _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _stream_of = raw or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _torch = torch
 
 
 def _enqueue(index, f, what, *args):

@@ -21,3 +21,25 @@ def test_arguments_inside_the_state_are_refused(abi, cache):  # noqa: F811
         assert f.semkv_paged_compact(c, far, 8, at(w), None) == -1, w
         assert f.semkv_paged_compact(c, at(w), 8, far, None) == -1, w
     assert f.semkv_paged_compact(c, at(sz.refs_word - 31), 8, far, None) == -1     # its last entry lies there
+
+
+def test_set_up_publishes_its_lookups_at_once(monkeypatch):
+    """A second thread's first call may look while the first one's is setting up:
+    it must find everything or nothing."""
+    import sys
+    import types
+    from paper_2608_28911_amd import paged
+    seen = []
+
+    class C:
+        def __getattr__(self, name):                     # every lookup that the set-up makes
+            seen.append(paged._torch)
+            return lambda *a: 0
+
+    for name in ("_torch", "_device", "_stream_of"):
+        monkeypatch.setattr(paged, name, None, raising=False)
+    fake = types.SimpleNamespace(_C=C(), cuda=C())
+    monkeypatch.setitem(sys.modules, "torch", fake)
+    paged._setup()
+    assert len(seen) >= 2 and all(t is None for t in seen)
+    assert paged._torch is fake and paged._device is not None and paged._stream_of is not None
