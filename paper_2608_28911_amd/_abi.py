@@ -104,10 +104,11 @@ def lib():
         # round, the process maps two runtimes and the library's launches do
         # not see torch's streams and allocations.
         import torch  # noqa: F401
-        _lib = ctypes.CDLL(LIB_PATH)
+        loaded = ctypes.CDLL(LIB_PATH)
         for name, (res, args) in EXPORTS.items():
-            f = getattr(_lib, name)
+            f = getattr(loaded, name)
             f.restype, f.argtypes = res, args
+        _lib = loaded                    # last: another thread may be looking
     return _lib
 
 

@@ -43,3 +43,28 @@ def test_set_up_publishes_its_lookups_at_once(monkeypatch):
     paged._setup()
     assert len(seen) >= 2 and all(t is None for t in seen)
     assert paged._torch is fake and paged._device is not None and paged._stream_of is not None
+
+
+def test_library_is_published_with_its_signatures(monkeypatch):
+    """Without them ctypes passes addresses as 32-bit integers: a second thread's
+    first call must not find the library before it has them all."""
+    from paper_2608_28911_amd import _abi
+    seen = []
+
+    class Function:
+        def __setattr__(self, name, value):
+            seen.append(_abi._lib)
+            object.__setattr__(self, name, value)
+
+    class Library:
+        def __init__(self, path):
+            self.f = {}
+
+        def __getattr__(self, name):
+            return self.f.setdefault(name, Function())
+
+    monkeypatch.setattr(_abi, "_lib", None)
+    monkeypatch.setattr(_abi.ctypes, "CDLL", Library)
+    got = _abi.lib()
+    assert len(seen) == 2 * len(_abi.EXPORTS) and all(x is None for x in seen)
+    assert _abi._lib is got and all(f.argtypes == _abi.EXPORTS[n][1] for n, f in got.f.items())
