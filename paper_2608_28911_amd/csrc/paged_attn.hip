@@ -27,13 +27,16 @@
 // whose issue slots are taken, beside 34 % of the matrix cores': 2048 tokens over
 // 16k 698 us, 836 TFLOP/s.
 //
-// Softmax: one pass with a running reference M per row.  It includes the
-// exponent of the largest V scale seen, so that w = 2^(x - M + 10) s_t lies
-// within fp16 whatever the scales; it is moved only when a record would pass
-// it by 2^5.  Scores, sums, the zeros' share and the accumulators are fp32;
-// w is rounded to fp16 (nearest), and the share that the rounding takes from
-// the middle of the codes' range (7.5) is given back through the zeros' sum,
-// which leaves an error relative to the values' spread within their group.
+// Softmax: one pass with a running reference M per row, the largest x + e of the
+// tokens that the row has seen, where 2^e bounds the token's V scale, so that w =
+// 2^(x - M + 10) s_t lies within fp16 whatever the scales; it is moved only when a
+// record would pass it by 2^5.  A token that the row does not see, or that is of
+// no weight, has no part in it, however large its V; of several channel groups
+// each has its scales taken relative to its own largest so far, 2^E_j.  Scores,
+// sums, the zeros' share and the accumulators are fp32; w is rounded to fp16
+// (nearest), and the share that the rounding takes from the middle of the codes'
+// range (7.5) is given back through the zeros' sum, which leaves an error relative
+// to the values' spread within their group.
 #include <hip/hip_fp16.h>
 
 #include "paged.h"
@@ -56,6 +59,7 @@ constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx
 // 65504), so that a weight (a sixteenth of it in every second slot) keeps its 11
 // bits down to 2^-20 of the largest
 constexpr float kHead = 10.0f, kLag = 5.0f;
+constexpr int kSpread = 5;                 // exponents of a page's V scales that lie close together (w keeps its bits to 2^-15 then)
 
 // 8 codes of a word as fp16: slots 0, 1, 4, 5 as c 2^-21, slots 2, 3, 6, 7 as c 2^-17
 constexpr float kCode = 0x1p21f;
@@ -87,16 +91,33 @@ __device__ inline float over_row(float x, F f) {
 __device__ inline float row_max(float x) { return over_row(x, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ inline float row_sum(float x) { return over_row(x, [](float a, float b) { return a + b; }); }
 
-// the largest of the wave's values: within 16 lanes by DPP moves, then as above
-__device__ inline uint32_t wave_max(uint32_t x) {
-  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0xB1, 0xF, 0xF, true)));    // lane xor 1
-  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x4E, 0xF, 0xF, true)));    // lane xor 2
-  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x141, 0xF, 0xF, true)));   // mirror of 8 lanes
-  x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x140, 0xF, 0xF, true)));   // mirror of 16
-  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = max(uint32_t(p[0]), uint32_t(p[1]));
-  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return max(uint32_t(q[0]), uint32_t(q[1]));
+// Ranges of V scales: the largest's fp16 bits in the lower half, and in the upper
+// one the negative of the smallest's, which is 0 for a scale of 0 (a token that
+// adds nothing) and the larger the smaller another one is.
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+__device__ inline ushort2v halves(uint32_t x) { return __builtin_bit_cast(ushort2v, x); }
+__device__ inline uint32_t word(ushort2v x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ inline uint32_t wider(uint32_t x, uint32_t y) { return word(__builtin_elementwise_max(halves(x), halves(y))); }
+__device__ inline uint32_t range_of(const uint32_t (&m)[4]) {     // of metadata words
+  const uint32_t a = __builtin_amdgcn_perm(m[1], m[0], 0x05040100u), b = __builtin_amdgcn_perm(m[3], m[2], 0x05040100u);
+  const uint32_t hi = wider(a, b), lo = wider(word(-halves(a)), word(-halves(b)));
+  return wider(__builtin_amdgcn_perm(lo, hi, 0x05040100u), __builtin_amdgcn_perm(lo, hi, 0x07060302u));
+}
+__device__ inline uint32_t range_over_16(uint32_t x) {            // of 16 lanes, by DPP moves
+  x = wider(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0xB1, 0xF, 0xF, true)));    // lane xor 1
+  x = wider(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x4E, 0xF, 0xF, true)));    // lane xor 2
+  x = wider(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x141, 0xF, 0xF, true)));   // mirror of 8 lanes
+  return wider(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x140, 0xF, 0xF, true)));   // mirror of 16
+}
+// e with scale < 2^e: at most twice too large, for subnormals up to 2^10 times
+__device__ inline int exponent_of(uint32_t scale) { return int(scale >> 10) - 14; }
+// the range of exponents e - kSpread to e
+__device__ inline uint32_t limits_of(int e) {
+  const uint32_t low = uint32_t(max(e + 14 - kSpread, 0)) << 10;
+  return uint32_t(e + 14) << 10 | 0x3FFu | (low ? 0x10000u - low : 0xFFFFu) << 16;
+}
+__device__ inline bool passes(uint32_t range, uint32_t limits) {
+  return word(__builtin_elementwise_sub_sat(halves(range), halves(limits))) != 0;
 }
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -234,6 +255,59 @@ __device__ inline void put_row(const PagedAttnArgs& a, const Tile& tl, int head,
   v *= L == 0.0f ? 0.0f : 1.0f / L;                // no token: zeros
   *reinterpret_cast<uint2*>(a.out + at * D + ch) = make_uint2(pack_out(v[0], v[1], a.bf16), pack_out(v[2], v[3], a.bf16));
   if (ch == 0 && a.lse) a.lse[at] = L == 0.0f ? -INFINITY : (M - kHead + __builtin_log2f(L)) * 0.69314718055994531f;
+}
+
+// What a wave knows of its pages' V scales.  E: exponents of the groups' scales by
+// which weights and sums are scaled (one group: none).  limits: range that a lane
+// expects of the scales it holds; at first that of values of ordinary size (2^-6
+// to 1), so that the first page needs no set-up.  bound: of the exponents within
+// the limits, less E.  apart: the present page's exponents differ by more than
+// kSpread.
+template <int NG>
+struct Scales {
+  int E[NG];
+  uint32_t limits;
+  float bound;
+  bool apart;
+};
+
+// Each group's V scales seldom leave the range that an earlier page set.  Where
+// they do, it is set anew, and E raised if need be.  FIRST: the lane that the
+// first group's range begins at, the next group's 16 lanes on; lanes that hold
+// none have limits that nothing passes.
+template <int NG, int NR, int NC, int FIRST>
+__device__ __forceinline__ void look(Scales<NG>& sc, uint32_t range, bool holds, int kg, float4v (&o)[NR][NC], float4v (&ws)[NR]) {
+  if (__builtin_expect(!__any(passes(range, sc.limits)), 1)) return;
+  range = range_over_16(range);
+  int most = -64, least = 64;                      // of the page's exponents, less E
+  float fall[NG];
+  bool rise = false;
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const uint32_t both = __builtin_amdgcn_readlane(range, FIRST + 16 * j);
+    const int hi = exponent_of(both & 0xFFFFu), lo = both >> 16 ? exponent_of(0x10000u - (both >> 16)) : 64;
+    fall[j] = __builtin_ldexpf(1.0f, min(sc.E[j] - hi, 0));
+    if (NG > 1 && hi > sc.E[j]) {
+      sc.E[j] = hi;
+      rise = true;
+    }
+    most = max(most, hi - sc.E[j]);
+    least = min(least, lo - sc.E[j]);
+    if (kg % NG == j) sc.limits = limits_of(hi);
+  }
+  if (!holds) sc.limits = ~0u;
+  if (rise) {                                      // the groups' sums so far are of the lower ones
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        ws[r] *= kg == j ? fall[j] : 1.0f;
+#pragma unroll
+        for (int ct = j * (NC / NG); ct < (j + 1) * (NC / NG); ++ct) o[r][ct] *= fall[j];
+      }
+  }
+  sc.bound = float(most);
+  sc.apart = most - least > kSpread;
 }
 
 // Partial of one split: each row's D sums, its M and l.
@@ -384,6 +458,13 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 
   float4v o[NR][NC], ws[NR];                       // ws: lane group kg holds group kg's (one group: every lane)
   float M[NR], l[NR], az[NR][NG];
+  // lanes whose metadata (of the last load) are V's
+  auto holds_v = [&] { return SHARE || (64 * (MV - 1) + lane >= 16 * NG && 64 * (MV - 1) + lane < META); };
+  Scales<NG> sc;
+#pragma unroll
+  for (int j = 0; j < NG; ++j) sc.E[j] = 0;
+  sc.limits = holds_v() ? limits_of(0) : ~0u;
+  sc.bound = 0.0f;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     M[r] = -INFINITY;
@@ -404,7 +485,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   for (int p = SHARE ? 0 : p0 + wave; p < p1; p += SHARE ? 1 : NW) {
     const auto rs = record(next);
     const int have = page < 0 ? 0 : tl.len;        // tokens of a missing page are past the end
-    uint32_t smax = 0;
+    uint32_t range = 0;                            // of the V scales that the lane holds
     const uint4* kmeta;                            // [group][tile][4 tokens of kg]
     if constexpr (SHARE) {
       __syncthreads();                             // page p is staged, page p - 1 has been used
@@ -417,29 +498,36 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
       }
       if (first >= tl.rows || p * kPage > last_seen) continue;
       kmeta = sm_meta[p & 1] + kg;
-      const uint4 m = sm_meta[p & 1][16 * NG + (lane & (16 * NG - 1))];
-      smax = max(max(m.x & 0xFFFFu, m.y & 0xFFFFu), max(m.z & 0xFFFFu, m.w & 0xFFFFu));
+      const uint4 mv = sm_meta[p & 1][16 * NG + (lane & (16 * NG - 1))];
+      const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
+      range = range_of(m);
     } else {
       page = next;
       next = page_at(p + 2 * NW);
       // a lane holds 4 tokens of a group, first K's groups, then V's.  V's for
       // tokens past the sequence's end, which may be anything, become 0; the
-      // largest V scale of the others enters the softmax's reference
+      // others' range enters the softmax's reference
 #pragma unroll
       for (int i = 0; i < MV; ++i) {
         const int at = 64 * i + lane, t = p * kPage + 4 * (at & 15);
         uint32_t m[4] = {mw[i].x, mw[i].y, mw[i].z, mw[i].w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (at >= 16 * NG) m[e] = t + e < have ? m[e] : 0u;
-          smax = max(smax, at >= 16 * NG && at < META ? m[e] & 0xFFFFu : 0u);
-        }
+        for (int e = 0; e < 4; ++e) m[e] = at < 16 * NG || t + e < have ? m[e] : 0u;
+        range = range_of(m);                       // the last load is V's
         if (META % 64 == 0 || at < META) sm_meta[wave][at] = make_uint4(m[0], m[1], m[2], m[3]);
       }
       wave_order();
       kmeta = sm_meta[wave] + kg;
     }
     const uint4* vmeta = kmeta + 16 * NG;
+
+    // (SHARE has nothing to load before the scores, which hide this look's wait
+    // for LDS: before them it costs a chunk 1 %, a prompt at D = 64 2.5 %.  With four
+    // groups it is the other way round)
+    constexpr bool kLookLate = SHARE && NG < 4;
+    constexpr int kFirstV = SHARE ? 0 : 16 * NG & 63;
+    sc.apart = false;
+    if constexpr (!kLookLate) look<NG, NR, NC, kFirstV>(sc, range, holds_v(), kg, o, ws);
 
     // scores (a wave with matrix instructions to issue goes first, here and from
     // the first 32 tokens' values on: without the latter 722 us instead of 698 for
@@ -495,9 +583,13 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
       }
     }
 
-    // the reference: row maximum plus the exponent of the record's largest V scale
-    smax = wave_max(smax);
-    const float se = float(int(smax >> 10)) - 14.0f;
+    if constexpr (kLookLate) look<NG, NR, NC, kFirstV>(sc, range, holds_v(), kg, o, ws);
+
+    // the page's part of the reference.  Where its exponents lie close together,
+    // the largest x plus their bound is at most 2^kSpread too large; else each
+    // token's own counts, of several groups (relative to E_j) the largest (where
+    // every page needs that: 2048 tokens over 16k 833 us, else 697; one token over
+    // 32k 15.4 and 14.3).
     float ref[NR];
     bool move = false;
     float cand[NR];
@@ -508,9 +600,31 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
       for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[r][tt][e]);
-      cand[r] = fmaf(row_max(mx), cf[r], se);
-      move |= cand[r] > M[r] + kLag;
+      cand[r] = fmaf(row_max(mx), cf[r], sc.bound);
     }
+    if (sc.apart) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) cand[r] = -INFINITY;
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        int ex[4] = {-64, -64, -64, -64};
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const uint4 mv = vmeta[j * 16 + tt * 4];
+          const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ex[e] = max(ex[e], exponent_of(m[e] & 0xFFFFu) - sc.E[j]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int r = 0; r < NR; ++r) cand[r] = fmaxf(cand[r], fmaf(x[r][tt][e], cf[r], float(ex[e])));
+      }
+#pragma unroll
+      for (int r = 0; r < NR; ++r) cand[r] = row_max(cand[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) move |= cand[r] > M[r] + kLag;
     if (__any(move)) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -531,6 +645,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     // weights of 32 tokens, then their products, twice: vector and matrix
     // instructions of a SIMD's two waves meet oftener (740 us became 698)
     const uint32_t* vd = reinterpret_cast<const uint32_t*>(vw);
+    float down[NG];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) down[j] = __builtin_ldexpf(1.0f, -sc.E[j]);
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       // sums of the rounded weights (of several groups, each in its own four
@@ -545,7 +662,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
           const uint32_t m[4] = {mv.x, mv.y, mv.z, mv.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float s = lo16(m[e]), mid = fmaf(7.5f, s, hi16(m[e])), ss = e & 2 ? s * 0.0625f : s;
+            const float s = lo16(m[e]), mid = fmaf(7.5f, s, hi16(m[e]));
+            const float ss = NG > 1 ? s * (e & 2 ? down[j] * 0.0625f : down[j]) : e & 2 ? s * 0.0625f : s;
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
               if (j == 0) {
@@ -582,6 +700,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
   // (the lane's number made anew: kept over the loop it would be spilled)
   const int lane2 = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)), tid = 64 * wave + lane2;
   const int n2 = lane2 & 15, kg2 = lane2 >> 4;
+  float up[NG];
+#pragma unroll
+  for (int j = 0; j < NG; ++j) up[j] = __builtin_ldexpf(1.0f, sc.E[j]);
   if constexpr (SHARE) {                           // the wave's rows are whole
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -589,12 +710,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         const float w = NG == 1 ? ws[r][0] : __shfl(ws[r][0], 16 * j + n2);
-        az[r][j] = fmaf(w, -7.5f * kSum, row_sum(az[r][j]));
+        az[r][j] = fmaf(w, -7.5f * kSum * up[j], row_sum(az[r][j]));
       }
       if (first + 16 * r + n2 >= tl.rows) continue;
 #pragma unroll
       for (int ct = 0; ct < NC; ++ct)
-        put_row<D>(a, tl, head, first + 16 * r + n2, 16 * ct + 4 * kg2, M[r], L, o[r][ct] * kCode + az[r][ct / CG]);
+        put_row<D>(a, tl, head, first + 16 * r + n2, 16 * ct + 4 * kg2, M[r], L, o[r][ct] * (kCode * up[ct / CG]) + az[r][ct / CG]);
     }
     return;
   }
@@ -608,7 +729,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     for (int j = 0; j < NG; ++j) {
       // the zeros' share, less what the rounded weights give to 7.5
       const float w = NG == 1 ? ws[r][0] : __shfl(ws[r][0], 16 * j + n2);
-      az[r][j] = fmaf(w, -7.5f * kSum, row_sum(az[r][j]));
+      az[r][j] = fmaf(w, -7.5f * kSum * up[j], row_sum(az[r][j]));
     }
     if (kg2 == 0) {
       sm_m[wave][16 * r + n2] = M[r];
@@ -630,7 +751,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_kernel(PagedAttnArgs a)
     if (16 * r + n2 < rows) {
 #pragma unroll
       for (int ct = 0; ct < NC; ++ct)
-        *reinterpret_cast<float4v*>(&sm_o[wave][n2][16 * ct + 4 * kg2]) = (o[r][ct] * kCode + az[r][ct / CG]) * f;
+        *reinterpret_cast<float4v*>(&sm_o[wave][n2][16 * ct + 4 * kg2]) = (o[r][ct] * (kCode * up[ct / CG]) + az[r][ct / CG]) * f;
     }
     __syncthreads();
     for (int at = tid; at < min(rows - 16 * r, 16) * LPR; at += NT) {

@@ -1,5 +1,6 @@
 """Calls of the paged 4-bit cache at the edges of what its header allows:
-arguments that are the cache's own buffers, malformed starts, missing pages.
+arguments that are the cache's own buffers, malformed starts, missing pages,
+values far apart in magnitude.
 Against the plain model of tests/pagedref.py; attention's tolerance is the one
 worked out in tests/test_gpu_paged.py."""
 import numpy as np
@@ -194,4 +195,98 @@ def test_compact_reports_tokens_of_missing_pages():
         assert not y[:, 1].any() and torch.equal(y[:, [0, 2, 3, 4]], x[:, [3, 140, 150, 219]])
     c.status_word.zero_()
     c.compact(ints([[0, 2], [1, 0]]), ints([2, 1]))      # every page is there now
+    assert c.status() == 0
+
+
+# --------------------------------------------------- values far in magnitude --
+
+def far_apart(c, lens, rng, large):
+    """Writes the sequences' tokens: small values, and where `large` says (bool
+    [n, head_dim], rows of all sequences) values up to fp16's range in V, whose
+    tokens are of no weight: their K lies against every q that
+    far_queries makes."""
+    import torch
+    n, h, d = sum(lens), c.cfg.n_kv_heads, c.cfg.head_dim
+    K = rng.standard_normal((n, h, d)).astype(np.float32)
+    V = rng.standard_normal((n, h, d)).astype(np.float32) * 1e-4
+    V = np.where(large[:, None], rng.uniform(-6e4, 6e4, V.shape).astype(np.float32), V)
+    K[large.all(1)] = -8.0
+    c.reserve(ints(lens + [0] * (c.cfg.max_seqs - len(lens))))
+    c.write(0, torch.from_numpy(K).half().cuda(), torch.from_numpy(V).half().cuda(), starts_of(lens))
+
+
+def far_queries(rng, n, heads, d, dtype):
+    import torch
+    q = 1.0 + 0.3 * rng.standard_normal((n, heads, d)).astype(np.float32)
+    return torch.from_numpy(q).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("d,g", [(128, 128), (128, 64), (128, 32), (64, 64), (64, 32)])
+def test_attn_large_values_of_unseen_and_weightless_tokens(d, g, shared):
+    """In every page one token's V is some 2^29 of the others'.  Its weight is
+    nothing to the rows that see it (e^-60), and the rows before it do not: the
+    others' weights must keep their bits for either."""
+    import torch
+    rng = np.random.default_rng(d + g + shared)
+    h, hq = (8, 64) if shared else (2, 8)
+    lens = [500, 300] if shared else [150, 90]
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=16, seqs=4, seq_pages=8)
+    large = np.concatenate([np.arange(n) % 64 == 50 for n in lens])
+    far_apart(c, lens, rng, np.repeat(large[:, None], d, 1))
+    n = sum(lens)
+    q = far_queries(rng, n, hq, d, torch.float16)
+    out, lse = c.attn(0, q, starts_of(lens), with_lse=True)
+    pick = (lambda t, hh: t % 13 == 0 and hh in (0, 29)) if shared else (lambda t, hh: (t + hh) % 3 == 0)
+    check_attn(c, lens, lens, q, out, lse, d ** -0.5, only=pick)
+    one = far_queries(rng, 2, hq, d, torch.float16)      # generation
+    out, lse = c.attn(0, one, starts_of([1, 1]), with_lse=True)
+    check_attn(c, lens, [1, 1], one, out, lse, d ** -0.5)
+    assert c.status() == 0
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("d,g", [(128, 64), (128, 32), (64, 32)])
+def test_attn_groups_far_apart(d, g, shared):
+    """Channel groups of V that differ by some 2^29: each keeps its own bits."""
+    import torch
+    rng = np.random.default_rng(d + g + shared + 7)
+    h, hq = (8, 64) if shared else (2, 8)
+    lens = [500, 300] if shared else [150, 90]
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=16, seqs=4, seq_pages=8)
+    n, groups = sum(lens), d // g
+    large = np.zeros((n, d), bool)
+    large[:, :g] = True                                  # the first group throughout
+    far_apart(c, lens, rng, large)
+    q = far_queries(rng, n, hq, d, torch.float16)
+    out, lse = c.attn(0, q, starts_of(lens), with_lse=True)
+    pick = (lambda t, hh: t % 13 == 0 and hh in (0, 29)) if shared else (lambda t, hh: (t + hh) % 3 == 0)
+    check_attn(c, lens, lens, q, out, lse, d ** -0.5, only=pick)
+    one = far_queries(rng, 2, hq, d, torch.float16)
+    out, lse = c.attn(0, one, starts_of([1, 1]), with_lse=True)
+    check_attn(c, lens, [1, 1], one, out, lse, d ** -0.5)
+    assert groups > 1 and c.status() == 0
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("d,g", [(128, 128), (128, 32), (64, 64)])
+def test_attn_values_of_every_magnitude(d, g, shared):
+    """V rows of 2^-13 to 2^13, in random order, then in ascending and in
+    descending order."""
+    import torch
+    rng = np.random.default_rng(d + g + shared + 9)
+    h, hq = (8, 64) if shared else (2, 8)
+    lens = [400, 300, 200] if shared else [150, 90, 200]
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=20, seqs=4, seq_pages=8)
+    n = sum(lens)
+    e = [rng.uniform(-13, 13, lens[0]), np.linspace(-13, 13, lens[1]), np.linspace(13, -13, lens[2])]
+    K = torch.from_numpy(rng.standard_normal((n, h, d)).astype(np.float32)).half().cuda()
+    V = torch.from_numpy((rng.standard_normal((n, h, d)) * 2.0 ** np.concatenate(e)[:, None, None]).astype(np.float32)).half().cuda()
+    c.reserve(ints(lens + [0]))
+    c.write(0, K, V, starts_of(lens))
+    pick = (lambda t, hh: t % 13 == 0 and hh in (0, 29)) if shared else (lambda t, hh: (t + hh) % 3 == 0)
+    for mul in (0.3, 3.0):
+        q = torch.from_numpy((rng.standard_normal((n, hq, d)) * mul).astype(np.float32)).to(torch.bfloat16).cuda()
+        out, lse = c.attn(0, q, starts_of(lens), with_lse=True)
+        check_attn(c, lens, lens, q, out, lse, d ** -0.5, only=pick)
     assert c.status() == 0
