@@ -290,3 +290,127 @@ def test_attn_values_of_every_magnitude(d, g, shared):
         out, lse = c.attn(0, q, starts_of(lens), with_lse=True)
         check_attn(c, lens, lens, q, out, lse, d ** -0.5, only=pick)
     assert c.status() == 0
+
+
+# ------------------------------------------------------- shapes at the ends --
+
+@pytest.mark.parametrize("h,gqa,d,g", [(1, 33, 64, 64), (2, 64, 128, 128), (2, 64, 64, 32), (8, 7, 128, 64), (150, 1, 64, 64),
+                                       (256, 2, 64, 32), (300, 1, 64, 64)])
+def test_attn_many_heads(h, gqa, d, g):
+    """A token's rows fill several tiles, tiles begin inside a token, and so many
+    kv heads that none is left a second workgroup: one token, a few, a chunk, over
+    contexts long enough to be split, beside slots without a row."""
+    import torch
+    rng = np.random.default_rng(h + gqa + d + g)
+    seqs = 6
+    lens = [1500, 40, 0, 700, 64, 3]
+    c = make(h=h, hq=h * gqa, d=d, g=g, n_pages=50, seqs=seqs, seq_pages=30)
+    fill(c, lens, rng)
+    for counts in ([1, 1, 1, 1, 1, 1], [1, 0, 0, 0, 0, 0], [3, 0, 0, 2, 0, 5], [0, 40, 0, 130, 0, 0]):
+        n = sum(counts)
+        q = rows(rng, (n, h * gqa, d), torch.float16) * 0.3
+        out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
+        step = max(1, n * h * gqa // 400)
+        check_attn(c, lens, counts, q, out, lse, d ** -0.5, only=lambda t, hh: (t * h * gqa + hh) % step == 0)
+        again = c.attn(0, q, starts_of(counts), with_lse=True)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    assert c.status() == 0 and not c.ws[:2 * 512 * 64].view(torch.int32).any()
+
+
+def test_attn_shared_decoding_with_seven_query_heads():
+    """Tiles of 128 rows whose waves begin inside a token."""
+    import torch
+    rng = np.random.default_rng(71)
+    c = make(h=8, hq=56, n_pages=40, seqs=4, seq_pages=12)
+    lens, counts = [600, 310, 90, 700], [600, 300, 95, 200]
+    fill(c, lens, rng)
+    q = rows(rng, (sum(counts), 56, 128), torch.bfloat16) * 0.3
+    out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
+    check_attn(c, lens, counts, q, out, lse, 128 ** -0.5, only=lambda t, h: (t * 56 + h) % 31 == 0 and t % 3 == 0)
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [7, 1, 20], [500, 300, 700]])
+def test_attn_over_its_own_queries(counts):
+    """out may be q itself."""
+    import torch
+    rng = np.random.default_rng(72)
+    c = make(h=8, hq=32, n_pages=90, seqs=3, seq_pages=70)
+    fill(c, [4000, 310, 900], rng)
+    q = rows(rng, (sum(counts), 32, 128), torch.float16) * 0.3
+    want = c.attn(0, q, starts_of(counts))
+    assert c.attn(0, q, starts_of(counts), out=q) is q
+    assert torch.equal(q, want)
+
+
+def test_pool_beyond_32_bits():
+    """Pages past 4 GiB of a pool: what the calls write, move, copy and read there
+    is what they do in a small one."""
+    import torch
+    shape = dict(n_layers=8, h=8, hq=32, g=32, seqs=4)
+    big, small = make(n_pages=7000, seq_pages=6980, **shape), make(n_pages=40, seq_pages=8, **shape)
+    assert big.pool.numel() > 1 << 32
+    got = []
+    for c, first in ((big, 6980), (small, 0)):
+        rng = np.random.default_rng(73)
+        table = np.full((4, c.cfg.seq_pages), -1, np.int32)
+        table[0, :5], table[1, :2] = first + np.array([4, 0, 19, 7, 2]), first + np.array([9, 1])
+        table[3, :first] = np.arange(first)              # the last slot holds the lower pages
+        c.assign(ints([300, 100, 0, 64 * first]), torch.from_numpy(table).cuda())
+        K, V = (rows(rng, (8, 400, 8, 128), torch.float16) for _ in range(2))
+        c.write(-1, K, V, starts_of([300, 100, 0]))
+        out = list(c.read(-1, starts_of([300, 100, 0]), 400))
+        q = rows(rng, (6, 32, 128), torch.float16) * 0.3
+        for layer in (0, 7):
+            out += c.attn(layer, q, starts_of([5, 1, 0]), with_lse=True)
+        c.fork(ints([0, 1, 0, 3]))
+        c.reserve(ints([1, 0, 1, 0]))
+        assert int(c.table[2, 4]) == first + 3           # the copy of the shared last page
+        k, v = (rows(rng, (8, 2, 8, 128), torch.float16) for _ in range(2))
+        c.write(-1, k, v, starts_of([1, 0, 1]))
+        keep = ints([list(range(0, 300, 3)), list(range(100)), [5] * 100, [0] * 100])
+        c.compact(keep, ints([100, -1, 7, -1]))
+        out += c.read(-1, starts_of([100, 100, 7]), 207)
+        assert c.status() == 0
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_attn_missing_pages_under_shared_decoding():
+    """As the other rows, to the same tolerance: a token of a missing page is not
+    there."""
+    import torch
+    rng = np.random.default_rng(74)
+    d, h, gq = 128, 8, 8
+    c = make(h=h, hq=h * gq, n_pages=60, seqs=4, seq_pages=16)
+    lens, counts = [500, 1, 900, 333], [500, 1, 300, 200]
+    fill(c, lens, rng)
+    table = c.table.clone()
+    table[0, 3], table[2, 2], table[3, 0], table[3, 5] = -1, -1, -1, -1
+    c.assign(c.lens, table)
+    q = rows(rng, (sum(counts), h * gq, d), torch.float16) * 0.3
+    out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
+    pool, table = c.pool.cpu().numpy().reshape(60, 1, h, -1), table.cpu().numpy()
+    u, eps, scale, at = 2.0 ** -24, 2.0 ** -11, d ** -0.5, 0
+    for s, m in enumerate(counts):
+        for i in range(0, m, 17):
+            t, n = at + i, lens[s] - m + i + 1
+            for hh in ((t * 5) % (h * gq), (t * 11 + 1) % (h * gq)):
+                parts = [[], [], [], [], [], []]
+                for col in range(-(-n // 64)):
+                    if table[s, col] < 0:
+                        continue
+                    k, v = R.unpack(pool[table[s, col], 0, hh // gq], d, d)
+                    for p, x in zip(parts, k + v):
+                        p.append(x[:min(64, n - 64 * col)].astype(np.float64))
+                qq, o, l = q[t, hh].cpu().double().numpy(), out[t, hh].cpu().double().numpy(), float(lse[t, hh])
+                if not parts[0]:
+                    assert not o.any() and l == -np.inf
+                    continue
+                kc, ks, kz, vc, vs, vz = (np.concatenate(p) for p in parts)     # scales and zeros [n, 1]
+                want, wl, p = R.attend(qq, kc * ks + kz, vc * vs + vz, len(kc), scale)
+                dx = (d + 8) * u * scale * (np.abs(qq) @ (15 * ks + np.abs(kz) + 0 * kc).T).max()
+                lim = (eps * np.abs(want) + 2.0 ** -11 * (p @ (vs * np.abs(vc - 7.5)))
+                       + (np.expm1(2 * dx) + (n + 16) * u) * (p @ (15 * vs + np.abs(vz) + 0 * vc))) * (1 + eps) + 2.0 ** -24
+                assert np.all(np.abs(o - want) <= lim), (s, i, hh)
+                assert abs(l - wl) <= dx + (n + 16) * u + 4 * u * abs(wl) + 2.0 ** -22, (s, i, hh)
+        at += m
