@@ -448,8 +448,8 @@ int semkv_paged_read(const semkv_paged* c, int32_t layer, void* K, void* V, int3
  * same dtype, contiguous [n_rows][n_q_heads][head_dim], 16-byte aligned, apart
  * from q or q itself where that is contiguous; lse: fp32 [n_rows][n_q_heads] or
  * NULL.  scale: positive and finite.  (A row's q enters the first product in
- * fp16, scaled to its largest value: exactly where its values lie within 2^15 of
- * that one, and off by at most 2^-36 of it where they are smaller.)
+ * fp16, scaled to its largest value: exactly where its values lie within 2^24 of
+ * that one, and off by at most 2^-35 of it where they are smaller.)
  * workspace: ws_bytes >= sizes.workspace_bytes, 16-byte aligned; calls that
  * overlap in time need one each. */
 int semkv_paged_attn(const semkv_paged* c, int32_t layer, const void* q, int32_t dtype, int64_t sT, int64_t sH,

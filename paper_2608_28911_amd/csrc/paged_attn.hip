@@ -888,18 +888,24 @@ int launch_rows(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t rows = (a.r.n_rows * a.gqa + a.r.n_seqs - 1) / a.r.n_seqs;   // of a sequence, on average
   // A workgroup of 8 waves for a single sequence: half as many splits to join
   // (one token over 32k tokens 14.9 us, with 4 waves 17.7); else of 4, two of
-  // which hide each other's beginnings and ends (8 x 4k tokens 14.1, 21.5)
-  // or where a sequence holds few pages at most (2k tokens 9.4, with 8 10.4)
+  // which hide each other's beginnings and ends (8 x 4k tokens 14.1, 21.5).  By
+  // the table's width, since the host knows no length: a short sequence in a wide
+  // table loses by it (2k tokens in a table of 512 pages 10.4, with 4 waves 9.4)
   if (rows <= 16 && a.r.n_seqs == 1 && a.c.seq_pages > 64) return launch<D, G, 1, 8>(a, s);
   if (rows <= 16) return launch<D, G, 1, 4>(a, s);
   // as above: 5 tokens of 4 x 32k, with 8 waves 35.5 us, with 4 42.6; 8 chunks
   // of 64 tokens, which fill the chip, 65.5 and 56.7
   if (rows * a.r.n_seqs * a.c.n_kv_heads <= 32 * 128) return launch<D, G, 2, 8>(a, s);
   // Decoding shared by a workgroup's waves, which make a tile of four times the
-  // rows, where such tiles give every compute unit two: 4 prompts of 1024
-  // tokens 79 us, 108 apart; a 2048-token chunk over 16k (512 workgroups) 736
-  // and 748; but 8 chunks of 64 tokens (128 workgroups) 126 and 59
-  if ((a.r.n_rows * a.gqa / 128 + a.r.n_seqs) * a.c.n_kv_heads >= 512) return launch<D, G, 2, 4, true>(a, s);
+  // rows and is not split, where such tiles give every compute unit two (4 prompts
+  // of 1024 tokens 84 us, 118 apart; a 2048-token chunk over 16k, 512 workgroups,
+  // 697 and 725; but 8 chunks of 64 tokens, 128 workgroups, 126 and 59) and are
+  // more than half full (64 x 20 tokens over 500 36 and 52, over 4k 164 and 159;
+  // 64 x 16 35 and 41, but 163 and 119; 64 x 5 over 500 28 and 21, over 8k 266 and
+  // 125).  By the average: the host knows no starts, and a call that is a large
+  // chunk and a few single tokens over long contexts is not recognised (2048 over
+  // 16k and 15 x 1 over 16k 1177, apart 865; the two in calls of their own 775)
+  if (rows > 64 && (a.r.n_rows * a.gqa / 128 + a.r.n_seqs) * a.c.n_kv_heads >= 512) return launch<D, G, 2, 4, true>(a, s);
   return launch<D, G, 2, 4>(a, s);
 }
 

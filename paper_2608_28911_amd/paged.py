@@ -193,7 +193,8 @@ class PagedKV4:
     def attn(self, layer, q, starts, scale=None, out=None, lse=None, with_lse=False, workspace=None):
         """Causal attention of the sequences' last tokens over their pages: q [n, n_q_heads, head_dim] (fp16 or bf16,
         a unit channel stride) -> out of q's shape and dtype; with_lse: (out, lse fp32 [n, n_q_heads]).  scale:
-        1/sqrt(head_dim) if not given.  Calls that overlap in time need a workspace each (like cache.ws, zeroed once)."""
+        1/sqrt(head_dim) if not given.  Calls that overlap in time need a workspace each (like cache.ws, zeroed once).
+        Large chunks and single tokens of other, long sequences are faster in a call of their own each."""
         import torch
         code = _code(q.dtype, "q")
         shape, st = q.shape, q.stride()

@@ -230,8 +230,8 @@ def test_attn_large_values_of_unseen_and_weightless_tokens(d, g, shared):
     import torch
     rng = np.random.default_rng(d + g + shared)
     h, hq = (8, 64) if shared else (2, 8)
-    lens = [500, 300] if shared else [150, 90]
-    c = make(h=h, hq=hq, d=d, g=g, n_pages=16, seqs=4, seq_pages=8)
+    lens = [700, 500] if shared else [150, 90]           # 75 tiles of 8 heads
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=24, seqs=4, seq_pages=12)
     large = np.concatenate([np.arange(n) % 64 == 50 for n in lens])
     far_apart(c, lens, rng, np.repeat(large[:, None], d, 1))
     n = sum(lens)
@@ -252,8 +252,8 @@ def test_attn_groups_far_apart(d, g, shared):
     import torch
     rng = np.random.default_rng(d + g + shared + 7)
     h, hq = (8, 64) if shared else (2, 8)
-    lens = [500, 300] if shared else [150, 90]
-    c = make(h=h, hq=hq, d=d, g=g, n_pages=16, seqs=4, seq_pages=8)
+    lens = [700, 500] if shared else [150, 90]           # 75 tiles of 8 heads
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=24, seqs=4, seq_pages=12)
     n, groups = sum(lens), d // g
     large = np.zeros((n, d), bool)
     large[:, :g] = True                                  # the first group throughout
@@ -276,8 +276,8 @@ def test_attn_values_of_every_magnitude(d, g, shared):
     import torch
     rng = np.random.default_rng(d + g + shared + 9)
     h, hq = (8, 64) if shared else (2, 8)
-    lens = [400, 300, 200] if shared else [150, 90, 200]
-    c = make(h=h, hq=hq, d=d, g=g, n_pages=20, seqs=4, seq_pages=8)
+    lens = [600, 300, 300] if shared else [150, 90, 200]
+    c = make(h=h, hq=hq, d=d, g=g, n_pages=24, seqs=4, seq_pages=12)
     n = sum(lens)
     e = [rng.uniform(-13, 13, lens[0]), np.linspace(-13, 13, lens[1]), np.linspace(13, -13, lens[2])]
     K = torch.from_numpy(rng.standard_normal((n, h, d)).astype(np.float32)).half().cuda()
@@ -327,6 +327,22 @@ def test_attn_shared_decoding_with_seven_query_heads():
     q = rows(rng, (sum(counts), 56, 128), torch.bfloat16) * 0.3
     out, lse = c.attn(0, q, starts_of(counts), with_lse=True)
     check_attn(c, lens, counts, q, out, lse, 128 ** -0.5, only=lambda t, h: (t * 56 + h) % 31 == 0 and t % 3 == 0)
+
+
+@pytest.mark.parametrize("m", [5, 16, 20])
+def test_attn_few_tokens_of_many_sequences(m):
+    """64 sequences' drafts: tiles of 128 rows would be less than half full, half
+    full, and more."""
+    import torch
+    rng = np.random.default_rng(75 + m)
+    lens = [int(x) for x in rng.integers(m, 400, 64)]
+    lens[10], lens[11], lens[63] = 1200, 3, 0
+    c = make(h=8, hq=32, d=64, g=64, n_pages=460, seqs=64, seq_pages=20)
+    fill(c, lens, rng)
+    q = rows(rng, (64 * m, 32, 64), torch.bfloat16) * 0.3
+    out, lse = c.attn(0, q, starts_of([m] * 64), with_lse=True)
+    check_attn(c, lens, [m] * 64, q, out, lse, 64 ** -0.5, only=lambda t, h: (t * 32 + h) % 23 == 0)
+    assert c.status() == 0
 
 
 @pytest.mark.parametrize("counts", [[1, 1, 1], [7, 1, 20], [500, 300, 700]])
@@ -382,7 +398,7 @@ def test_attn_missing_pages_under_shared_decoding():
     rng = np.random.default_rng(74)
     d, h, gq = 128, 8, 8
     c = make(h=h, hq=h * gq, n_pages=60, seqs=4, seq_pages=16)
-    lens, counts = [500, 1, 900, 333], [500, 1, 300, 200]
+    lens, counts = [500, 1, 900, 333], [500, 1, 400, 250]
     fill(c, lens, rng)
     table = c.table.clone()
     table[0, 3], table[2, 2], table[3, 0], table[3, 5] = -1, -1, -1, -1
