@@ -20,12 +20,15 @@
 // weights go from one product to the next in registers.
 //
 // What bounds it (8 kv heads of 128 channels, 4 query heads each, one group a
-// row): a batch of long contexts memory, 16 sequences of 8 to 16k tokens 49 us at
-// 4.5 TB/s; one sequence latency, 2k tokens 9.6 us, 32k 14.5 (by builds that leave
-// parts out, when it took 15 to 16: 2.5 with the launch until a workgroup knows its
-// tile, 5 for its pages, 2.7 to join the splits); chunks vector instructions, 66 % of
-// whose issue slots are taken, beside 34 % of the matrix cores': 2048 tokens over
-// 16k 698 us, 836 TFLOP/s.
+// row): a batch of long contexts memory, 16 sequences of 8 to 16k tokens 50 us, 4.4
+// TB/s (43 while their 218 MB stay in the last-level cache); one sequence latency,
+// 2k tokens 9.5 us, 32k 14.6 (by builds that leave parts out, when it took 15 to
+// 16: 2.5 with the launch until a workgroup knows its tile, 5 for its pages, 2.7 to
+// join the splits); chunks vector instructions, 65 % of whose issue slots are taken,
+// beside 34 % of the matrix cores': 2048 tokens over 16k 705 us, 828 TFLOP/s.  With
+// groups of 64 and 32 75 % and 82 % (847 and 1215 us), and at 64 channels 74 % (a
+// 4096-token prompt 130 us): a score takes the same vector instructions for half the
+// products, and each further group its own scale and zero.
 //
 // Softmax: one pass with a running reference M per row, the largest x + e of the
 // tokens that the row has seen, where 2^e bounds the token's V scale, so that w =
