@@ -438,11 +438,13 @@ int semkv_paged_read(const semkv_paged* c, int32_t layer, void* K, void* V, int3
  *   out = softmax(scale q . k_t) . v_t,  lse = ln sum_t exp(scale q . k_t)
  * over the values that semkv_paged_read gives.  A row that sees no token (an
  * empty sequence, missing pages) gives out 0 and lse -inf.
- * The weights p_t enter the second product in fp16, multiplied by V's scale s_t:
- * out is off by at most 2^-11 sum_t p_t s_t |c_t - 7.5| (c_t: V's code) and what
- * fp32 sums leave, whatever the tokens' magnitudes.  Only where a group's scale
- * of one token is some 2^15 times that of another, and the tokens' other groups
- * are not so far apart, do the smaller one's weights lose bits in that group.
+ * The weights p_t enter the second product in fp16, multiplied by V's scale s_t
+ * of the channel group: out is off by at most 2^-11 sum_t p_t s_t |c_t - 7.5|
+ * (c_t: V's code), by 2^-22 of the largest p_t s_t for each token that has less
+ * than 2^-15 of it, and by what fp32 sums leave, whatever magnitudes the tokens
+ * have (a scale below 2^-14 counts as 2^-14 here).  Of several groups the second
+ * bound is relative to the largest p_t s_t in any group, each group's scales taken
+ * relative to the largest of them in its sequence, or to 1 if none is larger.
  * q: element (row t, query head h, channel j) at t*sT + h*sH + j, dtype F16 or
  * BF16, 16-byte aligned, strides multiples of 8, |q| below 2^100; out: the
  * same dtype, contiguous [n_rows][n_q_heads][head_dim], 16-byte aligned, apart
