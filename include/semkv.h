@@ -426,6 +426,36 @@ int semkv_paged_compact(semkv_paged* c, const int32_t* keep, int64_t ld_keep, co
 int semkv_paged_write(semkv_paged* c, int32_t layer, const void* K, const void* V, int32_t dtype, int64_t sL, int64_t sT,
                       int64_t sH, const int32_t* starts, int32_t n_seqs, int64_t n_rows, hipStream_t stream);
 
+/* The rotation of rows by their positions, on the way into a cache.  Pair i of
+ * the first `dim` channels of a row at position p, (x, y), becomes
+ *   (x c - y s, y c + x s),  c = cos(p freqs[i]), s = sin(p freqs[i]):
+ * the angle is the product in 64 bits, c and s are rounded to fp32, then each
+ * product and each sum is.  (Angles below 2^31: c and s are within 2^-50 before
+ * they are rounded.)  Pair i: channels i and i + dim/2, or 2i and 2i+1 where
+ * interleaved is not 0; channels from dim on stay.
+ *  freqs:     device fp32 [dim/2].
+ *  positions: device int32 [n_rows], the row's position (tokens before it may
+ *             have been dropped from the cache); NULL: its place in its sequence.
+ *  dim:       a multiple of 16, at least 16, at most the row's channels. */
+typedef struct semkv_rotary {
+  const float* freqs;
+  const int32_t* positions;
+  int32_t dim, interleaved;
+} semkv_rotary;
+
+/* semkv_paged_write of one layer with the rotation on the way: K's rows are
+ * turned, and the turned rows (fp32) are quantized as above; V's are quantized as
+ * they are.  K and V as for semkv_paged_write.
+ * q: NULL, or the query rows beside them, element (row t, query head h, channel
+ * j) at t*qT + h*qH + j, turned alike and rounded to `dtype` once into q_out, at
+ * t*oT + h*oH + j: 16-byte aligned, strides multiples of 8.  q_out may be q itself
+ * (with q's strides); it overlaps no other argument, q included, otherwise.  A row
+ * that would precede its sequence's first token gives zeros; queries are turned also
+ * where writing is stalled or a page is missing. */
+int semkv_paged_append(semkv_paged* c, int32_t layer, const void* K, const void* V, int32_t dtype, int64_t sT, int64_t sH,
+                       const void* q, int64_t qT, int64_t qH, void* q_out, int64_t oT, int64_t oH, const semkv_rotary* rot,
+                       const int32_t* starts, int32_t n_seqs, int64_t n_rows, hipStream_t stream);
+
 /* The values that the pages hold for these rows: K and V contiguous
  * [n_rows][n_kv_heads][head_dim] (layer == -1: [n_layers] of them), dtype F16,
  * BF16 or F32, 16-byte aligned.  A row whose page is missing, or that would
@@ -457,6 +487,105 @@ int semkv_paged_read(const semkv_paged* c, int32_t layer, void* K, void* V, int3
 int semkv_paged_attn(const semkv_paged* c, int32_t layer, const void* q, int32_t dtype, int64_t sT, int64_t sH,
                      float scale, const int32_t* starts, int32_t n_seqs, int64_t n_rows, void* out, float* lse,
                      void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---- Paged cache of latents ---------------------------------------------
+ * For models whose heads share one latent vector a token, which is key and value
+ * to all of them, and a key part that is turned by the token's position: a token
+ * is those `latent` + `rope` values, in 16 bits as they are.  Pages, lengths,
+ * tables, the calls on them, rows, starts and status bits are those of the 4-bit
+ * cache above; so are the state's layout and the sizes.
+ *
+ *  n_heads: query heads, at most 128.  latent: 256 or 512.  rope: 32 or 64.
+ *  dtype:   SEMKV_DTYPE_F16 or _BF16: of the cache, and of every row.
+ *  n_pages, max_seqs, seq_pages: as above.
+ *  pool:    [n_pages][n_layers] records: [64][latent], then [64][rope].  Values
+ *           of tokens that are in use must be finite (semkv_latent_append sees to
+ *           it; a caller that fills the pool does).
+ *  workspace: scratch of semkv_latent_attn; needs no clearing. */
+typedef struct semkv_latent_config {
+  int32_t n_layers, n_heads, latent, rope, dtype;
+  int32_t n_pages, max_seqs, seq_pages;
+} semkv_latent_config;
+
+typedef struct semkv_latent {
+  semkv_latent_config cfg;
+  semkv_paged_sizes sz;
+  uint8_t* pool;    /* device, 16-byte aligned */
+  int32_t* state;   /* device, 16-byte aligned */
+  int32_t* status;  /* device status word */
+} semkv_latent;
+
+int semkv_latent_cache_sizes(const semkv_latent_config* cfg, semkv_paged_sizes* out);
+
+/* As semkv_paged_init, _assign, _reserve, _fork and _compact. */
+int semkv_latent_init(semkv_latent* c, const semkv_latent_config* cfg, void* pool, int32_t* state, int32_t* status,
+                      hipStream_t stream);
+int semkv_latent_assign(semkv_latent* c, const int32_t* lens, const int32_t* table, hipStream_t stream);
+int semkv_latent_reserve(semkv_latent* c, const int32_t* n_new, hipStream_t stream);
+int semkv_latent_fork(semkv_latent* c, const int32_t* parent, hipStream_t stream);
+int semkv_latent_compact(semkv_latent* c, const int32_t* keep, int64_t ld_keep, const int32_t* n_keep, hipStream_t stream);
+
+/* Rows into the pages of the sequences' last tokens: C (row t, channel j at
+ * t*cT + j, j < latent) as it is, R (t*rT + j, j < rope) turned by `rot` (dim at most
+ * rope) and rounded once; 16-byte aligned, strides multiples of 8.  q: NULL, or the
+ * queries' parts that meet R, turned likewise, as for semkv_paged_append (rope
+ * channels a head).  A token with a value that is not finite, also by the turn, is
+ * stored as zeros and sets SEMKV_STATUS_NONFINITE_KV.  Rows whose page is missing
+ * or held by another sequence too are not stored (SEMKV_STATUS_BAD_INDEX). */
+int semkv_latent_append(semkv_latent* c, int32_t layer, const void* C, int64_t cT, const void* R, int64_t rT, const void* q,
+                        int64_t qT, int64_t qH, void* q_out, int64_t oT, int64_t oH, const semkv_rotary* rot,
+                        const int32_t* starts, int32_t n_seqs, int64_t n_rows, hipStream_t stream);
+
+/* What the pages hold for these rows: C [n_rows][latent] and R [n_rows][rope],
+ * contiguous, 16-byte aligned, in the cache's type.  A row whose page is missing,
+ * or that would precede its sequence's first token, is zeros. */
+int semkv_latent_read(const semkv_latent* c, int32_t layer, void* C, void* R, const int32_t* starts, int32_t n_seqs,
+                      int64_t n_rows, hipStream_t stream);
+
+/* Causal attention of these rows, every head over the same tokens: row i of the m
+ * rows of a sequence of n tokens sees its tokens 0 .. n-m+i,
+ *   x_t = scale (q . c_t + q_rope . r_t), out = softmax(x) . c, lse = ln sum exp x
+ * with c_t the token's latent and r_t its key part.  A row that sees no token (an
+ * empty sequence, missing pages) gives out 0 and lse -inf.
+ * q: element (row t, head h, channel j) at t*qT + h*qH + j, j < latent; q_rope: at
+ * t*rT + h*rH + j, j < rope; the cache's dtype, 16-byte aligned, strides multiples of
+ * 8.  out: the same dtype, contiguous [n_rows][n_heads][latent], 16-byte aligned,
+ * apart from q_rope, and from q or q itself where that is contiguous; lse: fp32
+ * [n_rows][n_heads] or NULL.  scale: positive and finite.
+ * The weights p_t enter the second product rounded to the cache's type: out is off by
+ * at most 2^-8 (bf16) or 2^-11 (fp16) sum_t p_t |c_t|, in fp16 by 2^-35 of the
+ * largest weight times |c_t| for each token of less than 2^-24 of it, by what fp32
+ * sums leave, and by its own rounding.
+ * workspace: ws_bytes >= sizes.workspace_bytes, 16-byte aligned; calls that overlap
+ * in time need one each. */
+int semkv_latent_attn(const semkv_latent* c, int32_t layer, const void* q, int64_t qT, int64_t qH, const void* q_rope, int64_t rT,
+                      int64_t rH, float scale, const int32_t* starts, int32_t n_seqs, int64_t n_rows, void* out, float* lse,
+                      void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Beam search's choice, for `groups` searches of `width` beams: of a group's
+ * beams b (scores a_b: the sum of the log probabilities so far) and logits x_b,
+ * [groups][width] rows of `vocab` (dtype F16, BF16 or F32; element (g, b, i) at
+ * g*s_group + b*s_beam + i), the k candidates of the largest
+ *   t(b, i) = a_b + x_b[i] - ln sum_u exp(x_b[u]),
+ * in descending order, equal ones by lower beam, then lower token (rows' sums are
+ * joined, and t is worked out and compared, in 64 bits):
+ *   out_scores fp32 [groups][k]: t, rounded
+ *   parents int32 [groups][k]:   g * width + b: the slot, as semkv_paged_fork takes it
+ *   tokens int32 [groups][k]:    i
+ * scores: device fp32 [groups][width]; -inf: a beam that is not in use (a search's
+ * first step has one in use), whose logits are not read.  ended: NULL, or device
+ * int32 [groups][width]: a beam where it is not 0 has the one candidate (t = a_b,
+ * token `pad`), and its logits are not read.  A logit of -inf is no candidate; where
+ * there are fewer than k, the rest is -inf, -1, -1 (a fork empties those slots).  A
+ * beam in use without a finite sum (a NaN or +inf logit), or a score of NaN or +inf,
+ * makes its whole group NaN, -1, -1.
+ * width, k: 1 to 64; groups * width below 2^24, vocab below 2^31.
+ * workspace: device, semkv_beam_select_workspace() bytes, 16-byte aligned, needs no
+ * clearing. */
+int semkv_beam_select_workspace(int64_t groups, int32_t width, int64_t vocab, int32_t k, size_t* bytes);
+int semkv_beam_select(const void* logits, int32_t dtype, int64_t groups, int32_t width, int64_t vocab, int64_t s_group,
+                      int64_t s_beam, const float* scores, const int32_t* ended, int32_t pad, int32_t k, float* out_scores,
+                      int32_t* parents, int32_t* tokens, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* Log probabilities of given tokens (Sec. 3.3's self-information is their
  * negative), for [batch][T] rows of `vocab` logits x (dtype F16, BF16 or F32;

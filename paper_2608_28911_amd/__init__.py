@@ -12,7 +12,8 @@ from . import _abi
 from ._abi import BASE_AFFINE, BASE_ROT_AFFINE, BASE_TQ, SemKVError, check, lib
 
 __all__ = ["SemKVCache", "SemKVError", "BASE_AFFINE", "BASE_TQ", "BASE_ROT_AFFINE", "tq_codebook", "cache_sizes",
-           "score_hidden", "INDICATORS", "PagedKV4", "make_paged_config", "paged_sizes", "token_logprobs", "score_tokens"]
+           "score_hidden", "INDICATORS", "PagedKV4", "make_paged_config", "paged_sizes", "PagedLatent", "make_latent_config", "latent_sizes",
+           "beam_select", "token_logprobs", "score_tokens"]
 
 INDICATORS = {"delta_norm": _abi.IND_DELTA_NORM, "norm": _abi.IND_NORM, "variance": _abi.IND_VARIANCE,
               "cosine_delta": _abi.IND_COSINE_DELTA}
@@ -266,4 +267,5 @@ class SemKVCache:
         return self.pools[off:off + n * rb]
 
 
-from .paged import PagedKV4, make_paged_config, paged_sizes, score_tokens, token_logprobs  # noqa: E402
+from .paged import (PagedKV4, PagedLatent, beam_select, latent_sizes, make_latent_config, make_paged_config,  # noqa: E402
+                    paged_sizes, score_tokens, token_logprobs)

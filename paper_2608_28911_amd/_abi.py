@@ -53,6 +53,18 @@ class Paged(ctypes.Structure):
     _fields_ = [("cfg", PagedConfig), ("sz", PagedSizes), ("pool", vp), ("state", vp), ("status", vp)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("freqs", vp), ("positions", vp), ("dim", i32), ("interleaved", i32)]
+
+
+class LatentConfig(ctypes.Structure):
+    _fields_ = [(n, i32) for n in ("n_layers", "n_heads", "latent", "rope", "dtype", "n_pages", "max_seqs", "seq_pages")]
+
+
+class Latent(ctypes.Structure):
+    _fields_ = [("cfg", LatentConfig), ("sz", PagedSizes), ("pool", vp), ("state", vp), ("status", vp)]
+
+
 EXPORTS = {
     "semkv_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "semkv_cache_sizes": (ctypes.c_int, [ctypes.POINTER(Config), ctypes.POINTER(Sizes)]),
@@ -81,9 +93,24 @@ EXPORTS = {
     "semkv_paged_fork": (ctypes.c_int, [ctypes.POINTER(Paged), vp, vp]),
     "semkv_paged_compact": (ctypes.c_int, [ctypes.POINTER(Paged), vp, i64, vp, vp]),
     "semkv_paged_write": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, vp, i32, i64, i64, i64, vp, i32, i64, vp]),
+    "semkv_paged_append": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, vp, i32, i64, i64, vp, i64, i64, vp, i64, i64,
+                                          ctypes.POINTER(Rotary), vp, i32, i64, vp]),
     "semkv_paged_read": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, vp, i32, vp, i32, i64, vp]),
     "semkv_paged_attn": (ctypes.c_int, [ctypes.POINTER(Paged), i32, vp, i32, i64, i64, f32, vp, i32, i64, vp, vp, vp,
                                         sz, vp]),
+    "semkv_latent_cache_sizes": (ctypes.c_int, [ctypes.POINTER(LatentConfig), ctypes.POINTER(PagedSizes)]),
+    "semkv_latent_init": (ctypes.c_int, [ctypes.POINTER(Latent), ctypes.POINTER(LatentConfig), vp, vp, vp, vp]),
+    "semkv_latent_assign": (ctypes.c_int, [ctypes.POINTER(Latent), vp, vp, vp]),
+    "semkv_latent_reserve": (ctypes.c_int, [ctypes.POINTER(Latent), vp, vp]),
+    "semkv_latent_fork": (ctypes.c_int, [ctypes.POINTER(Latent), vp, vp]),
+    "semkv_latent_compact": (ctypes.c_int, [ctypes.POINTER(Latent), vp, i64, vp, vp]),
+    "semkv_latent_append": (ctypes.c_int, [ctypes.POINTER(Latent), i32, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64,
+                                           ctypes.POINTER(Rotary), vp, i32, i64, vp]),
+    "semkv_latent_read": (ctypes.c_int, [ctypes.POINTER(Latent), i32, vp, vp, vp, i32, i64, vp]),
+    "semkv_latent_attn": (ctypes.c_int, [ctypes.POINTER(Latent), i32, vp, i64, i64, vp, i64, i64, f32, vp, i32, i64, vp, vp,
+                                         vp, sz, vp]),
+    "semkv_beam_select_workspace": (ctypes.c_int, [i64, i32, i64, i32, ctypes.POINTER(sz)]),
+    "semkv_beam_select": (ctypes.c_int, [vp, i32, i64, i32, i64, i64, i64, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]),
     "semkv_token_logprobs_workspace": (ctypes.c_int, [i64, i64, i32, ctypes.POINTER(sz)]),
     "semkv_token_logprobs": (ctypes.c_int, [vp, i32, i32, i64, i64, i64, i64, vp, i64, i64, i32, vp, vp, i64, i64, i32,
                                             vp, vp, vp, sz, vp]),

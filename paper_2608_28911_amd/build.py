@@ -1,6 +1,6 @@
 """Build libsemkv.so (the C-ABI library of gfx950 HIP kernels) in-tree with hipcc.
 
-Quantizer and ranker objects are compiled with -ffp-contract=off and IEEE
+Quantizer, ranker and rotation objects are compiled with -ffp-contract=off and IEEE
 division/square root so their codes are bit-for-bit reproducible; all HIP code
 is compiled with packed-fp32 instructions disabled.
 """
@@ -30,7 +30,10 @@ SOURCES = {
     "paged.hip": ["-ffp-contract=off"],
     "paged_attn.hip": [],
     "paged_api.hip": [],
+    "latent.hip": ["-ffp-contract=off"],
+    "latent_attn.hip": [],
     "logprob.hip": [],
+    "beam.hip": [],
 }
 
 

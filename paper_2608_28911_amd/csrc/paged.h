@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "rotary.h"
+
 namespace semkv {
 
 constexpr int kPage = 64;        // tokens of a page
@@ -33,6 +35,7 @@ struct PagedView {
   int32_t* new_table;            // [max_seqs][seq_pages]
   int32_t* status;
   int32_t n_layers, n_kv_heads, n_pages, max_seqs, seq_pages, dim, group, record;
+  int32_t latent, rope;          // a cache of latents: their channels and the key part's; else 0
 };
 
 __device__ inline uint8_t* paged_record_at(const PagedView& c, int page, int layer, int head) {
@@ -54,6 +57,16 @@ struct PagedWriteArgs {
   int32_t layer0, layers, bf16, parts;
 };
 
+// Rows that are turned by their positions on the way: K's, and the queries' beside
+// them (q null: none).
+struct PagedAppendArgs {
+  PagedWriteArgs w;
+  RotaryArgs rot;
+  const uint16_t* q; uint16_t* q_out;
+  int64_t qT, qH, oT, oH;
+  int32_t gqa;
+};
+
 struct PagedReadArgs {
   PagedView c;
   PagedRows r;
@@ -70,6 +83,48 @@ struct PagedAttnArgs {
   float scale_log2e;
   uint16_t* out;
   float* lse;
+  float* ws;
+};
+
+// A cache of latents: rows of a latent vector C and a key part R, and the
+// queries' part that meets R.
+struct LatentAppendArgs {
+  PagedView c;
+  PagedRows r;
+  const uint16_t* C; const uint16_t* R;
+  int64_t cT, rT;
+  RotaryArgs rot;
+  const uint16_t* q; uint16_t* q_out;
+  int64_t qT, qH, oT, oH;
+  int32_t n_heads, layer, bf16;
+};
+
+struct LatentReadArgs {
+  PagedView c;
+  PagedRows r;
+  uint16_t* C; uint16_t* R;
+  int32_t layer;
+};
+
+struct LatentAttnArgs {
+  PagedView c;
+  PagedRows r;
+  const uint16_t* q; const uint16_t* q_rope;
+  int64_t qT, qH, rT, rH;
+  int32_t n_heads, layer, bf16, target;
+  float scale_log2e;
+  uint16_t* out;
+  float* lse;
+  float* ws;
+};
+
+struct BeamArgs {
+  const void* x;
+  int32_t dtype, width, k, pad, nsplit;
+  int64_t groups, vocab, s_group, s_beam;
+  const float* scores;
+  const int32_t* ended;
+  float* out_scores; int32_t* parents; int32_t* tokens;
   float* ws;
 };
 
@@ -115,6 +170,8 @@ __device__ inline SeqRows lane_rows(const PagedView& c, const PagedRows& r, int 
   return {a, ok ? b - a : 0};
 }
 
+constexpr int kBad = 4, kNoPages = 8, kNonfinite = 2;   // status bits
+
 // Starts that descend, or pass the rows there are.
 __device__ inline bool starts_bad(const PagedRows& r, int s) {
   const int32_t a = r.starts[s], b = r.starts[s + 1];
@@ -152,12 +209,67 @@ __device__ inline int find_tile(const PagedView& c, const PagedRows& r, int flat
   return -1;
 }
 
+// Pages that the last `count` of `len` tokens touch.
+__device__ inline int pages_touched(int len, int count) {
+  const int first = max(len - count, 0);
+  return len > first ? (len - 1) / kPage - first / kPage + 1 : 0;
+}
+
+// What a workgroup of write or read works on: one page of one sequence.
+struct PageWork {
+  int seq;                      // -1: none
+  int page;                     // page id, -1: missing
+  int lo, hi;                   // slots of the page that are rows of the call
+  int64_t row0;                 // row of slot 0 (of slot lo: row0 + lo)
+  int first;                    // place of slot 0 in the sequence
+};
+__device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int flat) {
+  PageWork k;
+  int tile;
+  const int lane = threadIdx.x & 63;
+  SeqRows m = {0, 0};
+  int len = 0;
+  k.seq = find_tile(c, r, flat, lane, [](int n, int count) { return pages_touched(n, count); }, tile, m, len);
+  k.page = -1;
+  k.lo = k.hi = 0;
+  k.row0 = 0;
+  k.first = 0;
+  if (k.seq < 0) return k;
+  const int first = max(len - m.count, 0);
+  const int col = first / kPage + tile;
+  k.page = c.table[int64_t(k.seq) * c.seq_pages + col];
+  k.first = col * kPage;
+  k.lo = max(first - col * kPage, 0);
+  k.hi = min(len - col * kPage, kPage);
+  k.row0 = int64_t(m.first) + (int64_t(col) * kPage - (len - m.count));
+  return k;
+}
+
+// Workgroups in x for a call of n_rows rows: every touched page holds a row.
+inline int64_t touched_bound(const PagedRows& r) {
+  const int64_t by_pages = r.n_rows / kPage + 2 * int64_t(r.n_seqs);
+  return r.n_rows < by_pages ? r.n_rows : by_pages;
+}
+
+// Starts that are no partition of rows, or rows before the first token.
+__device__ inline void check_rows(const PagedView& c, const PagedRows& r) {
+  for (int s = threadIdx.x; s < r.n_seqs; s += blockDim.x)
+    if (starts_bad(r, s) || r.starts[s + 1] - r.starts[s] > c.lens[s]) atomicOr(c.status, kBad);
+}
+
 int launch_paged_clear(const PagedView& c, int tables, hipStream_t s);
 int launch_paged_assign(const PagedView& c, const int32_t* lens, const int32_t* table, hipStream_t s);
 int launch_paged_reserve(const PagedView& c, const int32_t* n_new, hipStream_t s);
 int launch_paged_fork(const PagedView& c, const int32_t* parent, hipStream_t s);
 int launch_paged_compact(const PagedView& c, const int32_t* keep, int64_t ld, const int32_t* n_keep, hipStream_t s);
 int launch_paged_write(PagedWriteArgs a, hipStream_t s);
+int launch_paged_append(PagedAppendArgs a, hipStream_t s);
+int launch_latent_append(const LatentAppendArgs& a, hipStream_t s);
+int launch_latent_read(const LatentReadArgs& a, hipStream_t s);
+size_t latent_attn_workspace(int latent);
+int launch_latent_attn(LatentAttnArgs a, size_t ws_bytes, hipStream_t s);
+size_t beam_select_workspace(int64_t rows, int64_t vocab, int k);
+int launch_beam_select(BeamArgs a, hipStream_t s);
 int launch_paged_read(const PagedReadArgs& a, hipStream_t s);
 size_t paged_attn_workspace(int d);
 int launch_paged_attn(PagedAttnArgs a, size_t ws_bytes, hipStream_t s);

@@ -10,19 +10,13 @@
 // rows are written in 88 us (4.5 TB/s of rows in and records out) and read in 75
 // (5.2 TB/s); 15600 of 62000 tokens of 4 layers move in 77 us; one row of each of
 // 16 sequences is written in 3.5 us.
-#include <hip/hip_fp16.h>
-
 #include <type_traits>
 
 #include "paged.h"
+#include "rows.h"
 
 namespace semkv {
 namespace {
-
-constexpr int kBad = 4, kNoPages = 8, kNonfinite = 2;   // status bits
-
-__device__ inline float h2f(uint32_t b) { return __half2float(__ushort_as_half(uint16_t(b))); }
-__device__ inline uint32_t f2h(float f) { return __half_as_ushort(__float2half_rn(f)); }
 
 // ---- page tables ---------------------------------------------------------
 
@@ -354,52 +348,29 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedView c, const int3
   }
 }
 
+// The same for a cache of latents, whose tokens are whole rows.
+__global__ __launch_bounds__(256) void latent_move_kernel(PagedView c, const int32_t* keep, int64_t ld) {
+  const int s = blockIdx.y, layer = blockIdx.z;
+  if (!c.changed[s]) return;
+  const int n = c.new_lens[s], first = blockIdx.x * kPage;
+  if (first >= n) return;
+  uint4* out = reinterpret_cast<uint4*>(paged_record_at(c, c.list[c.base[s] + blockIdx.x], layer, 0));
+  const int wide = c.latent / 8, more = c.rope / 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int t = wave; t < kPage; t += 4) {
+    const int pos = first + t < n ? keep[s * ld + first + t] : -1;
+    const int p = pos >= 0 && pos < c.lens[s] ? c.table[int64_t(s) * c.seq_pages + pos / kPage] : -1;
+    if (p < 0 && first + t < n && layer == 0 && lane == 0) atomicOr(c.status, kBad);
+    const uint4* from = reinterpret_cast<const uint4*>(paged_record_at(c, max(p, 0), layer, 0));
+    uint4 v = make_uint4(0, 0, 0, 0), r = v;
+    if (p >= 0 && lane < wide) v = from[pos % kPage * wide + lane];
+    if (p >= 0 && lane < more) r = from[kPage * wide + pos % kPage * more + lane];
+    if (lane < wide) out[t * wide + lane] = v;
+    if (lane < more) out[kPage * wide + t * more + lane] = r;
+  }
+}
+
 // ---- rows ----------------------------------------------------------------
-
-// Pages that the last `count` of `len` tokens touch.
-__device__ inline int pages_touched(int len, int count) {
-  const int first = max(len - count, 0);
-  return len > first ? (len - 1) / kPage - first / kPage + 1 : 0;
-}
-
-// What a workgroup of write or read works on: one page of one sequence.
-struct PageWork {
-  int seq;                      // -1: none
-  int page;                     // page id, -1: missing
-  int lo, hi;                   // slots of the page that are rows of the call
-  int64_t row0;                 // row of slot 0 (of slot lo: row0 + lo)
-};
-__device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int flat) {
-  PageWork k;
-  int tile;
-  const int lane = threadIdx.x & 63;
-  SeqRows m = {0, 0};
-  int len = 0;
-  k.seq = find_tile(c, r, flat, lane, [](int n, int count) { return pages_touched(n, count); }, tile, m, len);
-  k.page = -1;
-  k.lo = k.hi = 0;
-  k.row0 = 0;
-  if (k.seq < 0) return k;
-  const int first = max(len - m.count, 0);
-  const int col = first / kPage + tile;
-  k.page = c.table[int64_t(k.seq) * c.seq_pages + col];
-  k.lo = max(first - col * kPage, 0);
-  k.hi = min(len - col * kPage, kPage);
-  k.row0 = int64_t(m.first) + (int64_t(col) * kPage - (len - m.count));
-  return k;
-}
-
-// Workgroups in x for a call of n_rows rows: every touched page holds a row.
-int64_t touched_bound(const PagedRows& r) {
-  const int64_t by_pages = r.n_rows / kPage + 2 * int64_t(r.n_seqs);
-  return r.n_rows < by_pages ? r.n_rows : by_pages;
-}
-
-// Starts that are no partition of rows, or rows before the first token.
-__device__ inline void check_rows(const PagedView& c, const PagedRows& r) {
-  for (int s = threadIdx.x; s < r.n_seqs; s += blockDim.x)
-    if (starts_bad(r, s) || r.starts[s + 1] - r.starts[s] > c.lens[s]) atomicOr(c.status, kBad);
-}
 
 // Group parameters as fp16, saturated, and a code against the stored pair.
 struct Affine {
@@ -419,19 +390,6 @@ struct Affine {
     return __builtin_amdgcn_cvt_pk_u8_f32(__builtin_amdgcn_fmed3f((x - zero) * inv, 0.0f, 15.0f), e, w);
   }
 };
-
-__device__ inline bool finite(float x) { return fabsf(x) < INFINITY; }     // false for NaN
-
-template <int BF>
-__device__ inline void unpack2(uint32_t d, float& a, float& b) {
-  if constexpr (BF) {
-    a = __uint_as_float(d << 16);
-    b = __uint_as_float(d & 0xFFFF0000u);
-  } else {
-    a = h2f(d & 0xFFFFu);
-    b = h2f(d >> 16);
-  }
-}
 
 // f over runs of N = 2, 4, 8, 16, 32 or 64 lanes, in all of them: DPP moves
 // within 16 lanes, rows of 16 exchanged in registers beyond.
@@ -472,14 +430,31 @@ __device__ inline bool all_of(bool ok) {
 // A page's only row of the call (a generated token): one wave, two channels a
 // lane.  A K word is four lanes'; a V word is one channel of 8 tokens, of which
 // the row's nibble is replaced.
-template <int D, int G, int BF>
-__device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uint8_t* rec, int z, int kv, int holders) {
+template <int D, int G, int BF, bool ROT>
+__device__ inline void write_row(const PagedWriteArgs& a, const RotaryArgs& rot, const PageWork& w, uint8_t* rec, int z, int kv,
+                                 int holders) {
   constexpr int CB = paged_code_bytes(D), KI = D / 32;
   const int lane = threadIdx.x & 63, head = blockIdx.y, slot = w.lo;
   const bool on = lane < D / 2;
   const int ch = on ? 2 * lane : 0;
   const uint16_t* X = kv ? a.V : a.K;
-  const uint32_t d = *reinterpret_cast<const uint32_t*>(X + int64_t(z) * a.sL + (w.row0 + slot) * a.sT + head * a.sH + ch);
+  const uint16_t* row = X + int64_t(z) * a.sL + (w.row0 + slot) * a.sT + head * a.sH;
+  const uint32_t d = *reinterpret_cast<const uint32_t*>(row + ch);
+  const bool turned = ROT && kv == 0 && ch < rot.dim;
+  const bool second = ch >= rot.dim / 2;             // of the halves, where those are the pairs
+  uint32_t other = 0;
+  float2 t0 = make_float2(0.0f, 0.0f), t1 = t0;
+  if (turned) {
+    const int32_t pos = position_of(rot, w, slot);
+    if (rot.interleaved) {
+      t0 = turn_of(pos, rot.freqs[ch / 2]);
+    } else {
+      const int pair = second ? ch - rot.dim / 2 : ch;
+      other = *reinterpret_cast<const uint32_t*>(row + (second ? pair : ch + rot.dim / 2));
+      t0 = turn_of(pos, rot.freqs[pair]);
+      t1 = turn_of(pos, rot.freqs[pair + 1]);
+    }
+  }
   uint32_t* words = reinterpret_cast<uint32_t*>(rec + kv * CB);
   const int xv = (ch / 16) * 2 + slot / 32;
   uint32_t* vw = words + ((xv >> 2) * 64 + ((slot >> 2) & 3) * 16 + (ch & 15)) * 4 + (xv & 3);
@@ -494,6 +469,18 @@ __device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uin
   }
   float x0, x1;
   unpack2<BF>(d, x0, x1);
+  if (turned) {
+    if (rot.interleaved) {
+      const float x = turned_x(x0, x1, t0);
+      x1 = turned_y(x0, x1, t0);
+      x0 = x;
+    } else {
+      float y0, y1;
+      unpack2<BF>(other, y0, y1);
+      x0 = second ? turned_y(y0, x0, t0) : turned_x(x0, y0, t0);
+      x1 = second ? turned_y(y1, x1, t1) : turned_x(x1, y1, t1);
+    }
+  }
   const bool ok = all_of<G / 2>(finite(x0) && finite(x1));
   const Affine q(min_over<G / 2>(fminf(x0, x1)), max_over<G / 2>(fmaxf(x0, x1)));
   const uint32_t c0 = ok ? q.code(x0, 0, 0u) : 0u, c1 = ok ? q.code(x1, 0, 0u) : 0u;
@@ -515,6 +502,47 @@ __device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uin
   }
 }
 
+// Channels at .. at + D/4 - 1 of a row, x, turned; `row` is the whole row in memory,
+// which holds the other halves of the pairs (the same lines again, from the L1).
+// A lane's channels from rot.dim on stay.
+template <int D, int BF>
+__device__ __forceinline__ void turn_lane(const RotaryArgs& rot, const uint16_t* row, const float2* turns, int at, float (&x)[D / 4]) {
+  constexpr int Q = D / 4;
+  if (rot.interleaved) {
+#pragma unroll
+    for (int i = 0; i < Q; i += 4) {
+      if (at + i >= rot.dim) break;
+      const float4 t = *reinterpret_cast<const float4*>(turns + (at + i) / 2);
+      const float a = turned_x(x[i], x[i + 1], make_float2(t.x, t.y)), b = turned_x(x[i + 2], x[i + 3], make_float2(t.z, t.w));
+      x[i + 1] = turned_y(x[i], x[i + 1], make_float2(t.x, t.y));
+      x[i + 3] = turned_y(x[i + 2], x[i + 3], make_float2(t.z, t.w));
+      x[i] = a;
+      x[i + 2] = b;
+    }
+    return;
+  }
+  const int half = rot.dim / 2;                          // a multiple of 8
+#pragma unroll
+  for (int i = 0; i < Q; i += 8) {
+    if (at + i >= rot.dim) break;
+    const bool second = at + i >= half;
+    const int pair = second ? at + i - half : at + i;
+    const uint4 o = *reinterpret_cast<const uint4*>(row + (second ? pair : pair + half));
+    const uint32_t d[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 t = *reinterpret_cast<const float4*>(turns + pair + 2 * e);
+      const float2 ta = make_float2(t.x, t.y), tb = make_float2(t.z, t.w);
+      float y0, y1;
+      unpack2<BF>(d[e], y0, y1);
+      float& x0 = x[i + 2 * e];
+      float& x1 = x[i + 2 * e + 1];
+      x0 = second ? turned_y(y0, x0, ta) : turned_x(x0, y0, ta);
+      x1 = second ? turned_y(y1, x1, tb) : turned_x(x1, y1, tb);
+    }
+  }
+}
+
 // One workgroup quantizes the rows of one (page, layer, kv head): K and then
 // V, or one of them (a.parts == 2, where there are few pages).
 // Four lanes own a token row, D/4 channels each (with 16 lanes a row, loads
@@ -524,18 +552,18 @@ __device__ inline void write_row(const PagedWriteArgs& a, const PageWork& w, uin
 // layout.  A page that the rows fill only in part keeps its other rows: K
 // words belong to one row, V words hold 8 tokens and are merged with what is
 // there.
-template <int D, int G, int BF>
-__global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
+template <int D, int G, int BF, bool ROT>
+__device__ __forceinline__ void write_page(const PagedWriteArgs& a, const RotaryArgs& rot, uint8_t* codes, float2* turns, int zblock,
+                                           int parts) {
   constexpr int Q = D / 4;                               // channels of a lane
   constexpr int LG = G / Q > 1 ? G / Q : 1;              // lanes of a group
   constexpr int GQ = Q / G > 1 ? Q / G : 1, N = Q / GQ;  // groups of a lane, channels of each
   constexpr int CB = paged_code_bytes(D), KI = D / 32, PITCH = D + 4;
-  __shared__ __align__(16) uint8_t codes[kPage * PITCH];
   const PagedView& c = a.c;
   const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
-  const int z = a.parts == 2 ? blockIdx.z >> 1 : blockIdx.z, layer = a.layer0 + z, head = blockIdx.y;
-  const int kv0 = a.parts == 2 ? blockIdx.z & 1 : 0, kv1 = a.parts == 2 ? kv0 : 1;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
+  const int z = parts == 2 ? zblock >> 1 : zblock, layer = a.layer0 + z, head = blockIdx.y;
+  const int kv0 = parts == 2 ? zblock & 1 : 0, kv1 = parts == 2 ? kv0 : 1;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && zblock == 0) check_rows(c, a.r);
   const int stalled = *c.stalled;
   const PageWork w = page_work(c, a.r, blockIdx.x);
   if (w.seq < 0 || stalled) return;
@@ -543,7 +571,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   uint8_t* rec = paged_record_at(c, max(w.page, 0), layer, head);
   if (w.hi - w.lo == 1) {
     const int kv = kv0 + (tid >> 6);               // a wave each
-    if (kv <= kv1) write_row<D, G, BF>(a, w, rec, z, kv, holders);
+    if (kv <= kv1) write_row<D, G, BF, ROT>(a, rot, w, rec, z, kv, holders);
     return;
   }
   // the rows are loaded before the page's holders are looked at; slots that
@@ -557,6 +585,12 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
     if (tid == 0) atomicOr(c.status, kBad);
     return;
   }
+  if constexpr (ROT) {
+    if (kv0 == 0) {
+      make_turns<D>(rot, w, turns);
+      __syncthreads();
+    }
+  }
   bool bad = false;
 #pragma unroll 1
   for (int kv = kv0; kv <= kv1; ++kv) {
@@ -567,6 +601,9 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
       const uint32_t d[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) unpack2<BF>(d[e], x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
+    }
+    if constexpr (ROT) {
+      if (kv == 0 && q * Q < rot.dim) turn_lane<D, BF>(rot, a.K + from - q * Q, turns + (mine ? slot : w.lo) * turns_pitch(D), q * Q, x);
     }
     if (kv < kv1) {                                      // V's row while K's is worked on
 #pragma unroll
@@ -627,6 +664,58 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
     }
   }
   if (bad) atomicOr(c.status, kNonfinite);
+}
+
+template <int D, int G, int BF>
+__global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
+  __shared__ __align__(16) uint8_t codes[kPage * (D + 4)];
+  write_page<D, G, BF, false>(a, RotaryArgs{}, codes, nullptr, blockIdx.z, a.parts);
+}
+
+// Rows before their sequence's first token have no position that the cache knows:
+// their queries are zeros.
+template <int D>
+__device__ inline void early_queries(const PagedAppendArgs& a, int head) {
+  if (threadIdx.x >= 64) return;
+  int reached = 0;
+  for (int s0 = 0; s0 < a.w.r.n_seqs; s0 += 64) {
+    int len;
+    const SeqRows m = lane_rows(a.w.c, a.w.r, s0, threadIdx.x, reached, len);
+    for (int i = 0; i < m.count - len; ++i)
+      for (int j = 0; j < a.gqa * D; j += 8)
+        *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + (head * a.gqa + j / D) * a.oH + j % D) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// Write with the rotation on the way.  The workgroups of one (page, kv head): K and
+// V as above, K turned before it is quantized, and one more for the queries of
+// that head.
+template <int D, int G, int BF>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
+  __shared__ __align__(16) uint8_t codes[kPage * (D + 4)];
+  __shared__ __align__(16) float2 turns[kPage * turns_pitch(D)];
+  if (int(blockIdx.z) < a.w.parts) {
+    write_page<D, G, BF, true>(a.w, a.rot, codes, turns, blockIdx.z, a.w.parts);
+    return;
+  }
+  const int head = blockIdx.y;
+  if (blockIdx.x == 0) early_queries<D>(a, head);
+  const PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
+  if (w.seq < 0) return;
+  make_turns<D>(a.rot, w, turns);
+  __syncthreads();
+  constexpr int UNITS = D / 16;
+  const int rows = w.hi - w.lo, n = rows * a.gqa * UNITS;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int u = i % UNITS, h = i / UNITS % a.gqa, slot = w.lo + i / (UNITS * a.gqa);
+    const int64_t row = w.row0 + slot, at = head * a.gqa + h;
+    uint4 v[2];
+    int c0, c1;
+    turn_unit<BF>(a.rot, a.q + row * a.qT + at * a.qH, turns + slot * turns_pitch(D), u, v, c0, c1);
+    uint16_t* to = a.q_out + row * a.oT + at * a.oH;
+    *reinterpret_cast<uint4*>(to + c0) = v[0];
+    *reinterpret_cast<uint4*>(to + c1) = v[1];
+  }
 }
 
 // One workgroup returns the rows of one (page, layer, kv head): the record
@@ -767,7 +856,8 @@ int launch_paged_compact(const PagedView& c, const int32_t* keep, int64_t ld, co
   if (pages > c.seq_pages) pages = c.seq_pages;
   if (pages > 0) {
     const dim3 grid(unsigned(pages), unsigned(c.max_seqs), unsigned(c.n_layers * c.n_kv_heads));
-    if (c.dim == 128) hipLaunchKernelGGL((paged_move_kernel<128>), grid, dim3(256), 0, s, c, keep, ld);
+    if (c.latent) hipLaunchKernelGGL(latent_move_kernel, grid, dim3(256), 0, s, c, keep, ld);
+    else if (c.dim == 128) hipLaunchKernelGGL((paged_move_kernel<128>), grid, dim3(256), 0, s, c, keep, ld);
     else hipLaunchKernelGGL((paged_move_kernel<64>), grid, dim3(256), 0, s, c, keep, ld);
   }
   hipLaunchKernelGGL(paged_install_kernel, table_grid(c), dim3(256), 0, s, c, 1);
@@ -793,6 +883,28 @@ int launch_paged_write(PagedWriteArgs a, hipStream_t s) {
   } else {
     if (a.c.group == 64) write_of<64, 64>(a, grid, s);
     else write_of<64, 32>(a, grid, s);
+  }
+  return done();
+}
+
+template <int D, int G>
+static void append_of(const PagedAppendArgs& a, dim3 grid, hipStream_t s) {
+  if (a.w.bf16) hipLaunchKernelGGL((paged_append_kernel<D, G, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_append_kernel<D, G, 0>), grid, dim3(256), 0, s, a);
+}
+
+int launch_paged_append(PagedAppendArgs a, hipStream_t s) {
+  const PagedView& c = a.w.c;
+  const int64_t bound = touched_bound(a.w.r);
+  a.w.parts = bound * c.n_kv_heads < 2048 ? 2 : 1;
+  const dim3 grid(unsigned(bound), unsigned(c.n_kv_heads), unsigned(a.w.parts + (a.q ? 1 : 0)));
+  if (c.dim == 128) {
+    if (c.group == 128) append_of<128, 128>(a, grid, s);
+    else if (c.group == 64) append_of<128, 64>(a, grid, s);
+    else append_of<128, 32>(a, grid, s);
+  } else {
+    if (c.group == 64) append_of<64, 64>(a, grid, s);
+    else append_of<64, 32>(a, grid, s);
   }
   return done();
 }
