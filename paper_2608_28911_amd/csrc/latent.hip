@@ -52,28 +52,41 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
     PageWork mine = w;
     mine.lo = lo;
     mine.hi = hi;
+    // a wave's rows, all loaded before the first is looked at
+    constexpr int ROWS = kPage / kParts / 4;
+    const bool holds = lane < LANES, turns_one = lane < units;
+    const Unit place = unit_of(a.rot, lane);
+    uint4 v[ROWS], p[ROWS][2];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int64_t row = w.row0 + min(lo + wave + 4 * k, hi - 1);
+      v[k] = p[k][0] = p[k][1] = make_uint4(0, 0, 0, 0);
+      if (holds) v[k] = reinterpret_cast<const uint4*>(a.C + row * a.cT)[lane];
+      if (turns_one) {
+        p[k][0] = *reinterpret_cast<const uint4*>(a.R + row * a.rT + place.at);
+        p[k][1] = *reinterpret_cast<const uint4*>(a.R + row * a.rT + place.bt);
+      }
+    }
     make_turns<64>(a.rot, mine, turns);
     __syncthreads();
     uint16_t* to = latent_at(c, w.page, a.layer);
-    for (int slot = lo + wave; slot < hi; slot += 4) {
-      const int64_t row = w.row0 + slot;
-      const bool holds = lane < LANES, turns_one = lane < units;
-      uint4 v = make_uint4(0, 0, 0, 0), p[2] = {v, v};
-      if (holds) v = reinterpret_cast<const uint4*>(a.C + row * a.cT)[lane];
-      int at = 0, bt = 0;
-      if (turns_one) turn_unit<BF>(a.rot, a.R + row * a.rT, turns + slot * turns_pitch(64), lane, p, at, bt);
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int slot = lo + wave + 4 * k;
+      if (slot >= hi) break;
+      if (turns_one) turn_unit<BF>(a.rot, turns + slot * turns_pitch(64), lane, p[k]);
       // a token with a value that is not finite is kept as zeros: a weight of 0
       // times it would be NaN in the sums of every row
-      const bool ok = !__any(!finite8<BF>(v) || !finite8<BF>(p[0]) || !finite8<BF>(p[1]));
+      const bool ok = !__any(!finite8<BF>(v[k]) || !finite8<BF>(p[k][0]) || !finite8<BF>(p[k][1]));
       if (!ok) {
-        v = p[0] = p[1] = make_uint4(0, 0, 0, 0);
+        v[k] = p[k][0] = p[k][1] = make_uint4(0, 0, 0, 0);
         if (lane == 0) atomicOr(c.status, kNonfinite);
       }
-      if (holds) reinterpret_cast<uint4*>(to + slot * L)[lane] = v;
+      if (holds) reinterpret_cast<uint4*>(to + slot * L)[lane] = v[k];
       if (turns_one) {
         uint16_t* r = to + kPage * L + slot * c.rope;
-        *reinterpret_cast<uint4*>(r + at) = p[0];
-        *reinterpret_cast<uint4*>(r + bt) = p[1];
+        *reinterpret_cast<uint4*>(r + place.at) = p[k][0];
+        *reinterpret_cast<uint4*>(r + place.bt) = p[k][1];
       }
     }
     return;
@@ -94,17 +107,7 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
   if (w.seq < 0) return;
   make_turns<64>(a.rot, w, turns);
   __syncthreads();
-  const int n = (w.hi - w.lo) * heads * units;
-  for (int i = tid; i < n; i += 256) {
-    const int u = i % units, h = h0 + i / units % heads, slot = w.lo + i / (units * heads);
-    const int64_t row = w.row0 + slot;
-    uint4 p[2];
-    int at, bt;
-    turn_unit<BF>(a.rot, a.q + row * a.qT + h * a.qH, turns + slot * turns_pitch(64), u, p, at, bt);
-    uint16_t* to = a.q_out + row * a.oT + h * a.oH;
-    *reinterpret_cast<uint4*>(to + at) = p[0];
-    *reinterpret_cast<uint4*>(to + bt) = p[1];
-  }
+  turn_queries<BF, turns_pitch(64)>(a.rot, w, a.q, a.qT, a.qH, a.q_out, a.oT, a.oH, h0, heads, units, turns);
 }
 
 // A wave a row: zeros where its page is missing.

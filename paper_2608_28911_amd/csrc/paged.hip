@@ -432,9 +432,9 @@ __device__ inline bool all_of(bool ok) {
 // the row's nibble is replaced.
 template <int D, int G, int BF, bool ROT>
 __device__ inline void write_row(const PagedWriteArgs& a, const RotaryArgs& rot, const PageWork& w, uint8_t* rec, int z, int kv,
-                                 int holders) {
+                                 int holders, int head) {
   constexpr int CB = paged_code_bytes(D), KI = D / 32;
-  const int lane = threadIdx.x & 63, head = blockIdx.y, slot = w.lo;
+  const int lane = threadIdx.x & 63, slot = w.lo;
   const bool on = lane < D / 2;
   const int ch = on ? 2 * lane : 0;
   const uint16_t* X = kv ? a.V : a.K;
@@ -508,37 +508,38 @@ __device__ inline void write_row(const PagedWriteArgs& a, const RotaryArgs& rot,
 template <int D, int BF>
 __device__ __forceinline__ void turn_lane(const RotaryArgs& rot, const uint16_t* row, const float2* turns, int at, float (&x)[D / 4]) {
   constexpr int Q = D / 4;
-  if (rot.interleaved) {
-#pragma unroll
-    for (int i = 0; i < Q; i += 4) {
-      if (at + i >= rot.dim) break;
-      const float4 t = *reinterpret_cast<const float4*>(turns + (at + i) / 2);
-      const float a = turned_x(x[i], x[i + 1], make_float2(t.x, t.y)), b = turned_x(x[i + 2], x[i + 3], make_float2(t.z, t.w));
-      x[i + 1] = turned_y(x[i], x[i + 1], make_float2(t.x, t.y));
-      x[i + 3] = turned_y(x[i + 2], x[i + 3], make_float2(t.z, t.w));
-      x[i] = a;
-      x[i + 2] = b;
-    }
-    return;
-  }
   const int half = rot.dim / 2;                          // a multiple of 8
 #pragma unroll
-  for (int i = 0; i < Q; i += 8) {
-    if (at + i >= rot.dim) break;
-    const bool second = at + i >= half;
-    const int pair = second ? at + i - half : at + i;
-    const uint4 o = *reinterpret_cast<const uint4*>(row + (second ? pair : pair + half));
-    const uint32_t d[4] = {o.x, o.y, o.z, o.w};
+  for (int i = 0; i < Q; i += 8) {                       // eight channels at a time
+    if (at + i < rot.dim) {
+      const bool second = !rot.interleaved && at + i >= half;
+      const int pair = rot.interleaved ? (at + i) / 2 : second ? at + i - half : at + i;
+      if (rot.interleaved) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float4 t = *reinterpret_cast<const float4*>(turns + pair + 2 * e);
-      const float2 ta = make_float2(t.x, t.y), tb = make_float2(t.z, t.w);
-      float y0, y1;
-      unpack2<BF>(d[e], y0, y1);
-      float& x0 = x[i + 2 * e];
-      float& x1 = x[i + 2 * e + 1];
-      x0 = second ? turned_y(y0, x0, ta) : turned_x(x0, y0, ta);
-      x1 = second ? turned_y(y1, x1, tb) : turned_x(x1, y1, tb);
+        for (int e = 0; e < 4; e += 2) {
+          const float4 t = *reinterpret_cast<const float4*>(turns + pair + e);
+          const float2 ta = make_float2(t.x, t.y), tb = make_float2(t.z, t.w);
+          const float a = turned_x(x[i + 2 * e], x[i + 2 * e + 1], ta), b = turned_x(x[i + 2 * e + 2], x[i + 2 * e + 3], tb);
+          x[i + 2 * e + 1] = turned_y(x[i + 2 * e], x[i + 2 * e + 1], ta);
+          x[i + 2 * e + 3] = turned_y(x[i + 2 * e + 2], x[i + 2 * e + 3], tb);
+          x[i + 2 * e] = a;
+          x[i + 2 * e + 2] = b;
+        }
+      } else {
+        // y of the pair is x c + (its other half) s, x the same with -s
+        const uint4 o = *reinterpret_cast<const uint4*>(row + (second ? pair : pair + half));
+        const uint32_t d[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 t = *reinterpret_cast<const float4*>(turns + pair + 2 * e);
+          const float sa = second ? t.y : -t.y, sb = second ? t.w : -t.w;
+          float y0, y1;
+          unpack2<BF>(d[e], y0, y1);
+          const float p0 = x[i + 2 * e] * t.x, p1 = x[i + 2 * e + 1] * t.z, q0 = y0 * sa, q1 = y1 * sb;
+          x[i + 2 * e] = p0 + q0;
+          x[i + 2 * e + 1] = p1 + q1;
+        }
+      }
     }
   }
 }
@@ -553,25 +554,21 @@ __device__ __forceinline__ void turn_lane(const RotaryArgs& rot, const uint16_t*
 // words belong to one row, V words hold 8 tokens and are merged with what is
 // there.
 template <int D, int G, int BF, bool ROT>
-__device__ __forceinline__ void write_page(const PagedWriteArgs& a, const RotaryArgs& rot, uint8_t* codes, float2* turns, int zblock,
-                                           int parts) {
+__device__ __forceinline__ void write_page(const PagedWriteArgs& a, const RotaryArgs& rot, const PageWork& w, uint8_t* codes, float2* turns,
+                                           int zblock, int parts, int head) {
   constexpr int Q = D / 4;                               // channels of a lane
   constexpr int LG = G / Q > 1 ? G / Q : 1;              // lanes of a group
   constexpr int GQ = Q / G > 1 ? Q / G : 1, N = Q / GQ;  // groups of a lane, channels of each
   constexpr int CB = paged_code_bytes(D), KI = D / 32, PITCH = D + 4;
   const PagedView& c = a.c;
   const int tid = threadIdx.x, slot = tid >> 2, q = tid & 3;
-  const int z = parts == 2 ? zblock >> 1 : zblock, layer = a.layer0 + z, head = blockIdx.y;
+  const int z = parts == 2 ? zblock >> 1 : zblock, layer = a.layer0 + z;
   const int kv0 = parts == 2 ? zblock & 1 : 0, kv1 = parts == 2 ? kv0 : 1;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && zblock == 0) check_rows(c, a.r);
-  const int stalled = *c.stalled;
-  const PageWork w = page_work(c, a.r, blockIdx.x);
-  if (w.seq < 0 || stalled) return;
   const int holders = c.refs[max(w.page, 0)];
   uint8_t* rec = paged_record_at(c, max(w.page, 0), layer, head);
   if (w.hi - w.lo == 1) {
     const int kv = kv0 + (tid >> 6);               // a wave each
-    if (kv <= kv1) write_row<D, G, BF, ROT>(a, rot, w, rec, z, kv, holders);
+    if (kv <= kv1) write_row<D, G, BF, ROT>(a, rot, w, rec, z, kv, holders, head);
     return;
   }
   // the rows are loaded before the page's holders are looked at; slots that
@@ -669,53 +666,58 @@ __device__ __forceinline__ void write_page(const PagedWriteArgs& a, const Rotary
 template <int D, int G, int BF>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   __shared__ __align__(16) uint8_t codes[kPage * (D + 4)];
-  write_page<D, G, BF, false>(a, RotaryArgs{}, codes, nullptr, blockIdx.z, a.parts);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(a.c, a.r);
+  const int stalled = *a.c.stalled;
+  const PageWork w = page_work(a.c, a.r, blockIdx.x);
+  if (w.seq < 0 || stalled) return;
+  write_page<D, G, BF, false>(a, RotaryArgs{}, w, codes, nullptr, blockIdx.z, a.parts, blockIdx.y);
 }
 
 // Rows before their sequence's first token have no position that the cache knows:
 // their queries are zeros.
 template <int D>
-__device__ inline void early_queries(const PagedAppendArgs& a, int head) {
+__device__ inline void early_queries(const PagedAppendArgs& a) {
   if (threadIdx.x >= 64) return;
   int reached = 0;
   for (int s0 = 0; s0 < a.w.r.n_seqs; s0 += 64) {
     int len;
     const SeqRows m = lane_rows(a.w.c, a.w.r, s0, threadIdx.x, reached, len);
     for (int i = 0; i < m.count - len; ++i)
-      for (int j = 0; j < a.gqa * D; j += 8)
-        *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + (head * a.gqa + j / D) * a.oH + j % D) = make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < a.gqa * a.w.c.n_kv_heads * D; j += 8)
+        *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + j / D * a.oH + j % D) = make_uint4(0, 0, 0, 0);
   }
 }
 
-// Write with the rotation on the way.  The workgroups of one (page, kv head): K and
-// V as above, K turned before it is quantized, and one more for the queries of
-// that head.
+// Write with the rotation on the way.  The workgroups of a page: for each kv head
+// its K, turned before it is quantized, and its V, as above; and as many for the
+// queries, each a share of the page's rows with every head, which lie together in
+// memory and turn alike (a share of the heads with every row instead: 217 us for
+// 76000 rows of 8 kv heads and 32 query heads of 64 channels, not 186).  Of those 186
+// us 63 are K's and V's (written without a turn 42), the rest the queries' (a copy of
+// them 110: memory); 2048 rows of 128 channels 12.7 us (K and V 10).  Several heads to
+// a workgroup, which would share their cosines, spill.
 template <int D, int G, int BF>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
+__global__ __launch_bounds__(256, D == 128 ? 3 : 5) void paged_append_kernel(PagedAppendArgs a) {
   __shared__ __align__(16) uint8_t codes[kPage * (D + 4)];
   __shared__ __align__(16) float2 turns[kPage * turns_pitch(D)];
   if (int(blockIdx.z) < a.w.parts) {
-    write_page<D, G, BF, true>(a.w, a.rot, codes, turns, blockIdx.z, a.w.parts);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(a.w.c, a.w.r);
+    const int stalled = *a.w.c.stalled;
+    const PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
+    if (w.seq < 0 || stalled) return;
+    write_page<D, G, BF, true>(a.w, a.rot, w, codes, turns, blockIdx.z, a.w.parts, blockIdx.y);
     return;
   }
-  const int head = blockIdx.y;
-  if (blockIdx.x == 0) early_queries<D>(a, head);
-  const PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
+  if (blockIdx.x == 0 && blockIdx.y == 0) early_queries<D>(a);
+  PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
   if (w.seq < 0) return;
+  const int rows = w.hi - w.lo, lo = w.lo, shares = gridDim.y;
+  w.hi = lo + rows * int(blockIdx.y + 1) / shares;
+  w.lo = lo + rows * int(blockIdx.y) / shares;
+  if (w.lo >= w.hi) return;
   make_turns<D>(a.rot, w, turns);
   __syncthreads();
-  constexpr int UNITS = D / 16;
-  const int rows = w.hi - w.lo, n = rows * a.gqa * UNITS;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int u = i % UNITS, h = i / UNITS % a.gqa, slot = w.lo + i / (UNITS * a.gqa);
-    const int64_t row = w.row0 + slot, at = head * a.gqa + h;
-    uint4 v[2];
-    int c0, c1;
-    turn_unit<BF>(a.rot, a.q + row * a.qT + at * a.qH, turns + slot * turns_pitch(D), u, v, c0, c1);
-    uint16_t* to = a.q_out + row * a.oT + at * a.oH;
-    *reinterpret_cast<uint4*>(to + c0) = v[0];
-    *reinterpret_cast<uint4*>(to + c1) = v[1];
-  }
+  turn_queries<BF, turns_pitch(D)>(a.rot, w, a.q, a.qT, a.qH, a.q_out, a.oT, a.oH, 0, a.w.c.n_kv_heads * a.gqa, D / 16, turns);
 }
 
 // One workgroup returns the rows of one (page, layer, kv head): the record

@@ -18,15 +18,17 @@ struct RotaryArgs {
   int32_t dim, interleaved;      // channels turned; pairs (2i, 2i+1), else (i, i + dim/2)
 };
 
-// cos and sin of p f, rounded to 32 bits.  The angle is reduced to [-pi/4, pi/4] by
-// two parts of pi/2 (exact products in fused multiply-adds: k has at most 31 bits),
-// then both series are summed as far as 64 bits reach: x^15/15! and x^16/16!, what
-// follows is below 5e-17.  Some 25 operations in 64 bits, a vector instruction
-// each at a quarter of the 32-bit rate: 64 pairs of a token cost as much as 7 KB
-// of traffic, and are shared by the heads.
+// cos and sin of p f, rounded to 32 bits.  k, the nearest whole number of quarter
+// turns, comes out of an addition that leaves no bits below the point (its lowest
+// bits say which quarter); the angle is reduced to [-pi/4, pi/4] by two parts of
+// pi/2 (exact products in fused multiply-adds: k has at most 31 bits), then both
+// series are summed as far as 64 bits reach: x^15/15! and x^16/16!, what follows is
+// below 5e-17.  Some 30 operations in 64 bits, at the rate of 32-bit ones.
 __device__ inline float2 turn_of(int32_t p, float f) {
+  constexpr double WHOLE = 6755399441055744.0;                        // 1.5 2^52
   const double theta = double(p) * double(f);
-  const double k = __builtin_rint(theta * 0.63661977236758134308);
+  const double t = __builtin_fma(theta, 0.63661977236758134308, WHOLE);
+  const double k = t - WHOLE;
   double r = __builtin_fma(-k, 1.5707963267948965580, theta);
   r = __builtin_fma(-k, 6.1232339957367658e-17, r);
   const double z = r * r;
@@ -47,9 +49,9 @@ __device__ inline float2 turn_of(int32_t p, float f) {
   c = __builtin_fma(c, z, 4.1666666666666666667e-2);                  //  1/4!
   c = __builtin_fma(c, z, -0.5);
   c = __builtin_fma(c, z, 1.0);
-  const int q = int(int64_t(k)) & 3;             // quarter turns; a frequency that is not finite leaves NaN in r
-  const double a = q & 1 ? s : c, b = q & 1 ? c : s;
-  return make_float2(float(q == 1 || q == 2 ? -a : a), float(q >= 2 ? -b : b));
+  const uint32_t q = uint32_t(__builtin_bit_cast(uint64_t, t));       // quarters, modulo 4; a frequency that is not finite leaves NaN in r
+  const float a = float(q & 1 ? s : c), b = float(q & 1 ? c : s);
+  return make_float2((q + 1) & 2 ? -a : a, q & 2 ? -b : b);
 }
 
 // The pair (x, y) turned.
