@@ -14,7 +14,7 @@
 namespace semkv {
 namespace {
 
-constexpr int kMostKept = 64, kMostBeams = 64;   // candidates of a group, its beams
+constexpr int kMostKept = 64;                    // candidates of a group (of 64 beams at most)
 
 // Partial of one split of a row: m and pad, S (64 bits), then the kept keys.
 __host__ __device__ constexpr int partial_words(int k) { return 4 + 2 * k; }
@@ -39,15 +39,22 @@ __device__ inline uint4 load_anywhere(const char* p) {
   return v;
 }
 
-// One workgroup takes a row, or a share of one where there are few.
+// One workgroup takes a row, or a share of one where there are few.  The pass only
+// sums and keeps each lane's largest logit; the k-th largest of these, over the
+// workgroup, bounds what it can keep, and the few lanes that reach it (k, and what
+// ties) are looked through again, a lane's vectors across the wave; what reaches the
+// bound is put in order by counting.  (A list kept on the way took 33 us for 256 rows
+// of 128000 fp16 logits and k = 8, half of its vector instructions insertions; now 18.9,
+// of which 12 go with the logits, 5.4 TB/s.)
 template <int DT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   constexpr int V = Elem<DT>::vec, NT = 64 * WAVES, U = 4;
   __shared__ Row sm[WAVES];
-  __shared__ uint32_t sm_hi[WAVES * kMostKept], sm_lo[WAVES * kMostKept];
+  __shared__ uint32_t sm_most[NT];
+  __shared__ uint32_t sm_hi[NT], sm_lo[NT];                  // a wave's candidates: 64 of them
+  __shared__ int sm_n[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
-  if (!reads_row(a, row)) return;
   const int64_t g = row / a.width;
   const char* x = static_cast<const char*>(a.x) + (g * a.s_group + (row - g * a.width) * a.s_beam) * Elem<DT>::size;
   // vectors from the row's first element on, wherever that lies: rows of the same
@@ -55,87 +62,141 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   const int64_t vecs = a.vocab / V;
   const int64_t v0 = vecs * blockIdx.y / a.nsplit, v1 = vecs * (blockIdx.y + 1) / a.nsplit;
   Row s = {kFloor, 0.0f};
-  Kept kept = {0u, 0u};
   const int k = a.k;
-  uint32_t last = 0;                     // order of the wave's last kept key
 
-  auto single = [&](int64_t i, bool valid) {
-    const float e = valid ? load1<DT>(x, i) : -INFINITY;
-    if (e > s.m) raise(s, e);
-    s.S += valid ? exp_of(e - s.m) : 0.0f;
-    keep_all(kept, valid, valid ? order_of(e) : 0u, ~uint32_t(i), k, lane);
-    last = __builtin_amdgcn_readlane(kept.hi, k - 1);
+  // what is behind the last whole vector
+  const int64_t tail = vecs * V + lane;
+  const bool ends = blockIdx.y + 1 == a.nsplit && wave == 0 && tail < a.vocab;
+  const float last = ends ? load1<DT>(x, tail) : -INFINITY;
+
+  uint4 next[U];
+  auto load = [&](int64_t v) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = v + u * NT;
+      if (at < v1) next[u] = load_anywhere<DT>(x + 16 * at);
+    }
   };
-  for (int64_t v = v0 + tid - lane; v < v1; v += NT * U) {   // wave-uniform bound
+  load(v0 + tid);
+  if (!reads_row(a, row)) return;                            // (looked at while the first logits come)
+  for (int64_t v = v0 + tid; v < v1; v += NT * U) {
     uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = v + lane + u * NT;
-      if (at < v1) w[u] = load_anywhere<DT>(x + 16 * at);
-    }
-    float e[U][V], mx[U];
+    for (int u = 0; u < U; ++u) w[u] = next[u];
+    load(v + NT * U);                                        // under way while these are looked at
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool valid = v + lane + u * NT < v1;
-      unpack<DT>(w[u], e[u]);
-      mx[u] = -INFINITY;
+      if (v + u * NT >= v1) break;
+      float e[V], p[V];
+      unpack<DT>(w[u], e);
+      float mx = e[0];
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (!valid) e[u][i] = -INFINITY;
-        mx[u] = fmaxf(mx[u], e[u][i]);
-      }
-      if (mx[u] > s.m) raise(s, mx[u]);
-      float p[V];
+      for (int i = 1; i < V; ++i) mx = fmaxf(mx, e[i]);
+      if (mx > s.m) raise(s, mx);
 #pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = exp_of(e[u][i] - s.m);
+      for (int i = 0; i < V; ++i) p[i] = exp_of(e[i] - s.m);
 #pragma unroll
       for (int d = V / 2; d > 0; d /= 2)
 #pragma unroll
         for (int i = 0; i < d; ++i) p[i] += p[i + d];
       s.S += p[0];
     }
-    uint32_t most = 0;
+  }
+  if (last > s.m) raise(s, last);
+  s.S += ends ? exp_of(last - s.m) : 0.0f;
+
+  // the bound: of the lanes' largest, in the order of their upper 16 bits
+  sm_most[tid] = order_of(s.m);
+  __syncthreads();
+  uint32_t most[WAVES], least = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) most = max(most, v + lane + u * NT < v1 ? order_of(mx[u]) : 0u);
-    if (__any(most > last)) {
-      // while the list fills, the lanes' maxima bound what it can end with
-      const uint32_t least = max(last, kth_order(most, k));
-      const float bound = least > order_of(-INFINITY) ? logit_of(least) : -INFINITY;
+  for (int w = 0; w < WAVES; ++w) most[w] = sm_most[64 * w + lane];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t at = v + lane + u * NT;
-        if (!__any(at < v1 && mx[u] >= bound)) continue;
+  for (int b = 31; b >= 16; --b) {
+    int n = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const bool may = at < v1 && e[u][i] >= bound;
-          if (__any(may)) keep_all(kept, may, order_of(e[u][i]), ~uint32_t(at * V + i), k, lane);
+    for (int w = 0; w < WAVES; ++w) n += __popcll(__ballot(most[w] >= (least | 1u << b)));
+    if (n >= k) least |= 1u << b;
+  }
+  const float bound = least > order_of(-INFINITY) ? logit_of(least) : kFloor;   // -inf is no candidate
+  // f(may, order, complemented index): every logit of this wave that reaches the bound
+  auto visit = [&](auto f) {
+    uint64_t who = __ballot(s.m >= bound);
+    while (who) {                                            // four lanes' vectors at a time
+      constexpr int B = 4;
+      int from[B];
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        from[i] = who ? __ffsll((unsigned long long)who) - 1 : -1;
+        who &= who - 1;
+      }
+      for (int64_t j0 = 0; v0 + 64 * wave + j0 * NT < v1; j0 += 64) {
+        uint4 w[B];
+        bool in[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          const int64_t at = v0 + 64 * wave + from[i] + (j0 + lane) * NT;
+          in[i] = from[i] >= 0 && at < v1;
+          if (in[i]) w[i] = load_anywhere<DT>(x + 16 * at);
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          if (from[i] < 0) break;
+          float e[V];
+          unpack<DT>(w[i], e);
+#pragma unroll
+          for (int d = 0; d < V; ++d) {
+            const bool may = in[i] && e[d] >= bound;
+            if (__any(may)) f(may, order_of(e[d]), ~uint32_t((v0 + 64 * wave + from[i] + (j0 + lane) * NT) * V + d));
+          }
         }
       }
-      last = __builtin_amdgcn_readlane(kept.hi, k - 1);
     }
+    if (__any(ends && last >= bound)) f(ends && last >= bound, order_of(last), ~uint32_t(tail));
+  };
+  int n = 0;
+  visit([&](bool may, uint32_t h, uint32_t l) {
+    const uint64_t m = __ballot(may);
+    const int at = n + int(__builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0)));
+    if (may && at < 64) {
+      sm_hi[64 * wave + at] = h;
+      sm_lo[64 * wave + at] = l;
+    }
+    n += __popcll(m);
+  });
+  if (n > 64) {                                              // ties: a list in order, of the first k
+    Kept kept = {0u, 0u};
+    visit([&](bool may, uint32_t h, uint32_t l) { keep_all(kept, may, h, l, k, lane); });
+    sm_hi[64 * wave + lane] = kept.hi;
+    sm_lo[64 * wave + lane] = kept.lo;
+    n = k;
   }
-
-  const int64_t tail = vecs * V;
-  if (blockIdx.y + 1 == a.nsplit && wave == 0) single(tail + lane, tail + lane < a.vocab);
+  if (lane == 0) sm_n[wave] = n;
 
   // the lanes' sums relative to the wave's maximum
   auto add = [](float p, float q) { return p + q; };
   raise(s, over_wave(s.m, [](float p, float q) { return fmaxf(p, q); }));
   s.S = over_wave(s.S, add);
   if (lane == 0) sm[wave] = s;
-  if (lane < k) {
-    sm_hi[wave * k + lane] = kept.hi;
-    sm_lo[wave * k + lane] = kept.lo;
-  }
   __syncthreads();
-  if (wave != 0) return;
-  for (int i = k; i < WAVES * k; i += 64) {                // the other waves' keys into wave 0's
-    const bool valid = i + lane < WAVES * k;
-    const uint32_t h = valid ? sm_hi[i + lane] : 0u, l = valid ? sm_lo[i + lane] : 0u;
-    keep_all(kept, valid, h, l, k, lane);
-  }
+  // every candidate counts those before it: its place
   uint32_t* p = reinterpret_cast<uint32_t*>(a.ws) + (row * a.nsplit + blockIdx.y) * partial_words(k);
-  if (lane == 0) {
+  const uint32_t h = sm_hi[tid], l = sm_lo[tid];
+  int place = 0, all = 0;
+  for (int w = 0; w < WAVES; ++w) {
+    const int c = sm_n[w];
+    all += c;
+    for (int i = 0; i < c; ++i) {
+      const uint32_t hi = sm_hi[64 * w + i], lo = sm_lo[64 * w + i];
+      place += hi > h || (hi == h && lo > l);
+    }
+  }
+  if (lane < n && place < k) {
+    p[4 + 2 * place] = h;
+    p[5 + 2 * place] = l;
+  }
+  for (int i = all + tid; i < k; i += NT) p[4 + 2 * i] = p[5 + 2 * i] = 0;
+  if (tid == 0) {
     float m = sm[0].m;
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w].m);
@@ -145,24 +206,20 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
     p[0] = __float_as_uint(m);
     *reinterpret_cast<double*>(p + 2) = S;
   }
-  if (lane < k) {
-    p[4 + 2 * lane] = kept.hi;
-    p[5 + 2 * lane] = kept.lo;
-  }
 }
 
-// One workgroup chooses a group's candidates: its waves join the rows' splits,
-// a row at a time each, and every kept candidate counts those before it in each
-// row's list, which is in order: its place.
-__global__ __launch_bounds__(256) void beam_choose_kernel(BeamArgs a) {
-  __shared__ double sm_t[kMostBeams * kMostKept];
-  __shared__ int32_t sm_v[kMostBeams * kMostKept];
+// One workgroup chooses a group's candidates: its waves (one for each beam, 16 at
+// most) join the rows' splits, and every kept candidate counts those before it in
+// each row's list, which is in order: its place.
+__global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
+  extern __shared__ double sm_t[];                   // [width][k]
+  int32_t* sm_v = reinterpret_cast<int32_t*>(sm_t + a.width * a.k);
   __shared__ int sm_bad, sm_n;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, threads = blockDim.x;
   const int64_t g = blockIdx.x;
   if (tid == 0) sm_bad = sm_n = 0;
   __syncthreads();
-  for (int b = wave; b < a.width; b += 4) {
+  for (int b = wave; b < a.width; b += threads >> 6) {
     const int64_t row = g * a.width + b;
     const float score = a.scores[row];
     double t = -INFINITY;
@@ -220,18 +277,22 @@ __global__ __launch_bounds__(256) void beam_choose_kernel(BeamArgs a) {
   __syncthreads();
   const bool bad = sm_bad != 0;
   const int n = bad ? 0 : sm_n;
-  for (int i = n + tid; i < k; i += 256) {           // fewer candidates than wanted
+  for (int i = n + tid; i < k; i += threads) {       // fewer candidates than wanted
     a.out_scores[g * k + i] = bad ? NAN : -INFINITY;
     a.parents[g * k + i] = -1;
     a.tokens[g * k + i] = -1;
   }
   if (bad) return;
-  for (int i = tid; i < a.width * k; i += 256) {
+  for (int i = tid; i < a.width * k; i += threads) {
     const double t = sm_t[i];
     if (!(t > -INFINITY)) continue;
     const int mine = i / k;
     int place = i - mine * k;                        // what is before it in its own list
-    for (int b = 0; b < a.width && place < k; ++b) {
+    if (a.width * k <= 128) {                        // few: all of them, rather than one read after another
+      place = 0;
+#pragma unroll 4
+      for (int j = 0; j < a.width * k; ++j) place += sm_t[j] > t || (sm_t[j] == t && j < i);
+    } else for (int b = 0; b < a.width && place < k; ++b) {
       if (b == mine) continue;
       int lo = 0, hi = k;                            // entries before: larger, or equal and of a lower beam
       while (lo < hi) {
@@ -249,8 +310,10 @@ __global__ __launch_bounds__(256) void beam_choose_kernel(BeamArgs a) {
   }
 }
 
-// Splits of a row: enough workgroups for the chip where there are few rows,
-// each with 8192 logits at least.
+// Splits of a row: enough workgroups for the chip where there are few rows, each
+// with 8192 logits at least: a workgroup's fixed part (launch, first logits, bound,
+// second look, order) is 7 us.  (1024 workgroups for 256 rows of 128000: 26.2 us a
+// call instead of 25.0, 2048: 28.6.)
 int splits(int64_t rows, int64_t vocab) {
   int64_t n = 512 / rows;
   if (n > vocab / 8192) n = vocab / 8192;
@@ -270,7 +333,8 @@ int launch_beam_select(BeamArgs a, hipStream_t s) {
   if (a.dtype == 0) hipLaunchKernelGGL((beam_rows_kernel<0, 4>), grid, dim3(256), 0, s, a);
   else if (a.dtype == 1) hipLaunchKernelGGL((beam_rows_kernel<1, 4>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((beam_rows_kernel<2, 4>), grid, dim3(256), 0, s, a);
-  hipLaunchKernelGGL(beam_choose_kernel, dim3(unsigned(a.groups)), dim3(256), 0, s, a);
+  const int waves = a.width < 16 ? a.width : 16;
+  hipLaunchKernelGGL(beam_choose_kernel, dim3(unsigned(a.groups)), dim3(64 * waves), size_t(a.width) * a.k * 12, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
