@@ -16,6 +16,8 @@
 // of it.
 #include <hip/hip_fp16.h>
 
+#include <type_traits>
+
 #include "paged.h"
 
 namespace semkv {
@@ -26,7 +28,8 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kUnit = 32;                  // tokens of a unit
-constexpr int kSlots = 512, kMostSplits = 64, kLeast = 2;   // workgroups that units are shared out to, splits of a tile, units of a split
+constexpr int kBlock = 1024 + 32;          // bytes of LDS for 1 KB of latents
+constexpr int kSlots = 512, kMostSplits = 128, kLeast = 2;   // workgroups that units are shared out to, splits of a tile, units of a split
 constexpr int kTileWords = 4;              // words of a tile's description
 constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx9 family)
 constexpr float kLag = 5.0f;
@@ -74,11 +77,18 @@ __device__ inline float over_wave(float x, F f) {
   return over_row(x, f);
 }
 
-__device__ inline int wave_sum(int x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return __builtin_amdgcn_readfirstlane(x);
+// Sums of the lanes up to each one, by DPP moves: within rows of 16 lanes, then each
+// row's last sum into the next rows.
+__device__ inline int scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);     // lane - 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);     // lane - 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);     // lane - 4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);     // lane - 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // lane 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);    // lane 31 into rows 2 and 3
+  return x;
 }
+__device__ inline int wave_sum(int x) { return __builtin_amdgcn_readlane(scan(x), 63); }
 
 // What a workgroup works on: a tile of a sequence's rows of (token, head), and a
 // share of the units that it sees.
@@ -93,8 +103,8 @@ struct Tile {
 
 // The units of a call are shared out by what the sequences really hold, so that
 // no more workgroups are made than wanted (a.target; a partial each): a share is
-// the call's tiles times units over the wanted workgroups, and grows until they
-// suffice.  Where sequences pass 64, or that does not settle, so many are wanted
+// the call's tiles times units over the wanted workgroups, at least what makes a
+// split worth its joining, and grows until they suffice.  Where sequences pass 64, or that does not settle, so many are wanted
 // less the tiles: each tile's last share is the only one that is not full.
 // Consecutive shares of one split go to tiles of the same units: the workgroups
 // of an XCD (every eighth) take consecutive ones, and find each other's units in
@@ -114,21 +124,25 @@ __device__ inline Tile tile_of(const LatentAttnArgs& a, int block, int lane) {
   int reached = 0;
   Share mine = share(0, reached);
   const int reached64 = reached;
-  int64_t work = int64_t(mine.tiles) * mine.units;
+  // (below 2^30 where it is used: fewer than kSlots tiles of 2^21 units at most)
+  uint32_t work = uint32_t(mine.tiles) * uint32_t(mine.units);
   int tiles = mine.tiles;
   for (int s0 = 64; s0 < a.r.n_seqs; s0 += 64) {
     const Share k = share(s0, reached);
-    work += int64_t(k.tiles) * k.units;
+    work += uint32_t(k.tiles) * uint32_t(k.units);
     tiles += k.tiles;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+  work = uint32_t(wave_sum(int(work)));
   tiles = wave_sum(tiles);
-  const uint32_t wl = __builtin_amdgcn_readfirstlane(int(work)), wh = __builtin_amdgcn_readfirstlane(int(work >> 32));
-  const bool far = wh || wl >> 31 || a.target <= tiles;        // many tiles: a workgroup each
-  int chunk = INT32_MAX / 2;
-  if (!far) {
-    auto even = [&](int n) { return max(int((wl + uint32_t(n) - 1u) / uint32_t(n)), kLeast); };
+  int chunk = INT32_MAX / 2;                                   // many tiles: a workgroup each
+  if (tiles < a.target) {
+    // A split costs its partial's way to memory and back (64 rows of 512 channels 50 ns
+    // beside all others', 16 rows 13) where a unit takes a workgroup 2 us: of units u a
+    // split and W in all, u 2 us + W/u 50 ns is least at u^2 = W 50 ns / 2 us.  (8
+    // sequences of 2048 tokens with 128 heads 36 us without this, 29; 16 with 16 heads
+    // 22 and 18.)
+    const int least = max(kLeast, int(__builtin_sqrtf(float(work) * (ROWS == 64 ? 0.04f : 0.02f))));
+    auto even = [&](int n) { return max(int((work + uint32_t(n) - 1u) / uint32_t(n)), least); };
     chunk = even(a.target);
     bool fits = false;
     if (a.r.n_seqs <= 64) {
@@ -158,15 +172,7 @@ __device__ inline Tile tile_of(const LatentAttnArgs& a, int block, int lane) {
   for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
     if (s0) mine = share(s0, reached);
     const int splits = splits_of(mine.units), n = mine.tiles * splits;
-    int incl = n, tincl = mine.tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(incl, d), tup = __shfl_up(tincl, d);
-      if (lane >= d) {
-        incl += up;
-        tincl += tup;
-      }
-    }
+    const int incl = scan(n), tincl = scan(mine.tiles);
     const uint64_t above = __ballot(before + incl > flat);
     if (above) {
       const int l = __ffsll((unsigned long long)above) - 1;
@@ -196,20 +202,35 @@ __device__ inline Tile tile_of(const LatentAttnArgs& a, int block, int lane) {
   return k;
 }
 
-// Where 16 bytes (chunk) of a token's row lie in LDS: rotated within 256 bytes by
-// the token, so that 16 tokens' same chunk, and the eight tokens whose 32 bytes a
-// transposing read takes together, lie in different banks.
+// Where 16 bytes (chunk) of a token's row lie in LDS.  Latents: in blocks of 1 KB, as a
+// load leaves them (a token of 512, two of 256), a block 32 bytes further round the
+// banks than the one before; of two tokens in a block the second's chunks have bit 3
+// changed.  So the 16 lanes that a 16-byte read takes at once (0 to 3, 12 to 15, 20 to
+// 27 of each half wave, and the rest: eight tokens' chunk c, eight others' c + 1), and
+// the 32 that a transposing read does (eight tokens in a row, 32 bytes each), read
+// different banks, and channels further on are a constant further on.  (With blocks
+// 16 bytes apart the reads conflict: 53 million cycles of it in a chunk of 512 tokens,
+// 6 as it is.)  Key
+// parts: rotated by the token.
 template <int L>
-__device__ inline int latent_place(int t, int chunk) { return t * 2 * L + ((chunk ^ (t & 15)) << 4); }
+__host__ __device__ constexpr int latents_bytes() { return kUnit * L / 512 * kBlock; }
+template <int L>
+__device__ inline int latent_place(int t, int chunk) {
+  if constexpr (L == 512) return t * kBlock + (chunk << 4);
+  else return (t >> 1) * kBlock + (t & 1) * 512 + ((chunk ^ (t & 1) << 3) << 4);
+}
 template <int RP>
 __device__ inline int rope_place(int t, int chunk) {
   return t * 2 * RP + ((chunk ^ (RP == 64 ? (t >> 1) & 7 : (t >> 2) & 3)) << 4);
 }
 
+// The same for a row's weights, 16 bytes for each lane group: 5 % of a chunk's time.
+__device__ inline int weights_place(int row, int group) { return group ^ (row >> 3 << 1); }
+
 // The second product's operand of latents has channels along lanes and tokens in a
 // lane: 16 lanes read 8 bytes each, four tokens' 16 channels, and get them turned
 // (lane i: channel i of the four tokens).  Lane group g's elements are tokens
-// 8 g + 2 j, then 8 g + 2 j + 1.
+// 16 (g div 2) + 4 (g mod 2) + j, then those + 8.
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v lds_short4v;
 __device__ inline uint2 turned4(const uint8_t* p) {
@@ -224,6 +245,9 @@ typedef __attribute__((address_space(3))) void lds_void;
 // have it wait; they go elsewhere.  Counted by meet().
 __device__ inline void put_lds(void* p, uint32_t v) {
   __asm__ volatile("ds_write_b32 %0, %1" : : "v"(uint32_t(uintptr_t((lds_void*)p))), "v"(v) : "memory");
+}
+__device__ inline void put_lds(void* p, uint2 v) {
+  __asm__ volatile("ds_write_b64 %0, %1" : : "v"(uint32_t(uintptr_t((lds_void*)p))), "v"(uint64_t(v.y) << 32 | v.x) : "memory");
 }
 __device__ inline void put_lds(void* p, float v) { put_lds(p, __float_as_uint(v)); }
 
@@ -240,26 +264,29 @@ __device__ inline int anew(int x) {
   return x;
 }
 
-// A unit from its record straight into LDS, 1 KB a wave's load.  Lane i's 16 bytes
-// go to chunk i of the 64 chunks; from which chunk it takes them makes the places above.
+// A unit from its record straight into LDS, 1 KB a wave's load; from which chunk a
+// lane takes its 16 bytes makes the places above.
 template <int L, int RP>
 __device__ __forceinline__ void load_unit(const PagedView& c, int layer, int page, int half, int most, int wave, int lane, uint8_t* sm_c,
                                           uint8_t* sm_r) {
   constexpr int PER = 512 / L, N = kUnit / (4 * PER);      // tokens of a load, loads of a wave
   const uint8_t* rec = paged_record_at(c, page, layer, 0);
   const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(rec), 0, 2 * kPage * (L + RP), kBufferWord3);
+  const int sub = PER > 1 ? lane >> 5 : 0, at = ((lane & (L / 8 - 1)) ^ sub << 3) << 4;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int t = (4 * i + wave) * PER + (PER > 1 ? lane >> 5 : 0), ch = lane & (L / 8 - 1);
-    const int from = (half * kUnit + min(t, most)) * 2 * L, at = (ch ^ (t & 15)) << 4;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(sm_c + (4 * i + wave) * 1024), 16, PER > 1 ? from + at : at,
-                                             PER > 1 ? 0 : __builtin_amdgcn_readfirstlane(from), 0, 0);
+    const int block = 4 * i + wave;
+    uint8_t* to = sm_c + block * kBlock;
+    if constexpr (PER == 1)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)to, 16, at, (half * kUnit + min(block, most)) * 2 * L, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)to, 16, min(2 * block + sub, most) * 2 * L + at, half * kUnit * 2 * L, 0, 0);
   }
   if (wave * 1024 < kUnit * RP * 2) {
     constexpr int CH = RP / 8;
-    const int t = wave * (64 / CH) + lane / CH, ch = lane & (CH - 1);
-    const int at = (half * kUnit + min(t, most)) * 2 * RP + ((ch ^ (RP == 64 ? (t >> 1) & 7 : (t >> 2) & 3)) << 4);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(sm_r + wave * 1024), 16, at, 2 * kPage * L, 0, 0);
+    const int t = wave * (64 / CH) + lane / CH, rc = lane & (CH - 1);
+    const int rat = min(t, most) * 2 * RP + ((rc ^ (RP == 64 ? (t >> 1) & 7 : (t >> 2) & 3)) << 4);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(sm_r + wave * 1024), 16, rat, 2 * kPage * L + half * kUnit * 2 * RP, 0, 0);
   }
 }
 
@@ -267,10 +294,11 @@ template <int L, int RP, int BF, int RT>
 __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   constexpr int ROWS = 16 * RT, KL = L / 32, KR = RP / 32, CT = L / 64, NQ = RT == 4 ? 2 : 1;   // NQ: token tiles of a wave's scores
   constexpr float HEAD = head_of(BF);
-  __shared__ __align__(1024) uint8_t sm_c0[kUnit * L * 2], sm_c1[kUnit * L * 2];
-  __shared__ __align__(1024) uint8_t sm_r0[kUnit * RP * 2], sm_r1[kUnit * RP * 2];
+  __shared__ __align__(64) uint8_t sm_c0[latents_bytes<L>()], sm_c1[latents_bytes<L>()];
+  __shared__ __align__(64) uint8_t sm_r0[kUnit * RP * 2], sm_r1[kUnit * RP * 2];
   __shared__ __align__(16) uint4 sm_p[ROWS][4];
   __shared__ float sm_max[2][ROWS], sm_alpha[ROWS], sm_l[2][ROWS], sm_m[ROWS];
+  __shared__ __align__(16) uint32_t sm_moved[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   const PagedView& c = a.c;
   if (blockIdx.x == gridDim.x - 1)
@@ -325,29 +353,31 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
 #pragma unroll
     for (int k = 0; k < CT; ++k) o[r][k] = float4v{0, 0, 0, 0};
   float M = -INFINITY, l = 0.0f;
-  // places that the lane reads: of its token's chunks g, g + 4, ... (every fourth
-  // lies 256 bytes on), and of the channels that transposing reads take
-  const int vt = 8 * g + 2 * (n >> 2), vs = ((n >> 1) & 1) ^ (vt & 15);
-  const int qat = latent_place<L>(n, g), vat = vt * 2 * L + (((2 * CT * wave) ^ vs) << 4) + 8 * (n & 1);
+  // places that the lane reads: of its token's chunk g (every fourth further on is
+  // 64 bytes further on, but for bit 3), and what it takes for the transposing reads
+  const int qat = latent_place<L>(n, g), qat8 = latent_place<L>(n, g + 8) - 128;    // L == 512: the same
+  const int vat = latent_place<L>(16 * (g >> 1) + 4 * (g & 1) + (n >> 2), 2 * CT * wave + ((n >> 1) & 1)) + 8 * (n & 1);
+  if (tid < 4) sm_moved[tid] = 0;
 
   auto step = [&](const uint8_t* sm_c, const uint8_t* sm_r, uint8_t* next_c, uint8_t* next_r) __attribute__((always_inline)) {
     meet_loaded();
     const int at = u;
     u = next;
-    if (u < u1) load(u, next_c, next_r);
     const int after = table[min(u + 1, u1 - 1) >> 1];
+    if (u < u1) load(u, next_c, next_r);
 
     float4v x[NQ];
     float mx = -INFINITY;
     if (scores) {
-      const int qp = anew(qat), tile = 16 * tt0;
+      __builtin_amdgcn_s_setprio(1);
+      const int tile = 16 * tt0;
 #pragma unroll
       for (int j = 0; j < NQ; ++j) x[j] = float4v{0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KL; ++k)
 #pragma unroll
         for (int j = 0; j < NQ; ++j)
-          x[j] = mfma<BF>(*reinterpret_cast<const uint4*>(sm_c + (qp ^ (k & 3) << 6) + (k >> 2) * 256 + (tile + 16 * j) * 2 * L), q[k], x[j]);
+          x[j] = mfma<BF>(*reinterpret_cast<const uint4*>(sm_c + (L == 512 || !(k & 2) ? qat : qat8) + k * 64 + (tile + 16 * j) * (kBlock * L / 512)), q[k], x[j]);
 #pragma unroll
       for (int k = 0; k < KR; ++k)
 #pragma unroll
@@ -362,8 +392,7 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x100, NQ, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * NQ, 0);
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) x[j] *= a.scale_log2e;
+      __builtin_amdgcn_s_setprio(0);
       if (at * kUnit + kUnit - 1 > all_see) {
 #pragma unroll
         for (int j = 0; j < NQ; ++j)
@@ -375,7 +404,7 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
       for (int j = 0; j < NQ; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[j][e]);
-      mx = row_max(mx);
+      mx = row_max(mx) * a.scale_log2e;
     }
     if constexpr (RT < 4) {                               // two waves hold a row's tokens
       if (scores && g == 0) put_lds(&sm_max[tt0][16 * rt0 + n], mx);
@@ -393,15 +422,18 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = exp2_fast(x[j][e] - ref);
+          p[e] = exp2_fast(fmaf(x[j][e], a.scale_log2e, -ref));
           l += p[e];
         }
         // tokens 16 (tt0 + j) + 4 g + e, in the order of turned4
-        uint32_t* to = reinterpret_cast<uint32_t*>(&sm_p[16 * rt0 + n][2 * (tt0 + j) + (g >> 1)]);
-        put_lds(to + (g & 1), pack2<BF>(p[0], p[2]));
-        put_lds(to + 2 + (g & 1), pack2<BF>(p[1], p[3]));
+        put_lds(reinterpret_cast<uint2*>(&sm_p[16 * rt0 + n][weights_place(n, 2 * (tt0 + j) + (g & 1))]) + (g >> 1),
+                make_uint2(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3])));
       }
-      if (g == 0 && tt0 == 0) put_lds(&sm_alpha[16 * rt0 + n], alpha);
+      if (tt0 == 0) {                                      // rows whose reference has moved
+        const bool moved = __any(alpha != 1.0f);
+        if (moved && g == 0) put_lds(&sm_alpha[16 * rt0 + n], alpha);
+        if (lane == 0) put_lds(&sm_moved[rt0], moved ? 1u : 0u);
+      }
     }
     meet();
     page = after;
@@ -409,24 +441,22 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
     if (page < 0) next = find(u + 1);
 
     uint4 p[RT];
-    float alpha[RT];
-    bool moved = false;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      p[r] = sm_p[16 * r + n][g];
-      alpha[r] = sm_alpha[16 * r + n];
-      moved = moved || alpha[r] != 1.0f;
+    for (int r = 0; r < RT; ++r) p[r] = sm_p[16 * r + n][weights_place(n, g)];
+    const uint4 moved = *reinterpret_cast<const uint4*>(sm_moved);
+    if (__builtin_amdgcn_readfirstlane(RT == 1 ? moved.x : moved.x | moved.y | moved.z | moved.w)) {
+      const uint32_t which[4] = {moved.x, moved.y, moved.z, moved.w};
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float alpha = which[r] ? sm_alpha[16 * r + n] : 1.0f;
+#pragma unroll
+        for (int k = 0; k < CT; ++k) o[r][k] *= alpha;
+      }
     }
-    if (__any(moved)) {
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int k = 0; k < CT; ++k) o[r][k] *= alpha[r];
-    }
-    const int vp = anew(vat);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < CT; ++k) {
-      const uint2 lo = turned4(sm_c + (vp ^ k << 5)), hi = turned4(sm_c + (vp ^ (k << 5 | 16)) + 2 * L);
+      const uint2 lo = turned4(sm_c + vat + 32 * k), hi = turned4(sm_c + vat + 8 * (kBlock * L / 512) + 32 * k);
       const uint4 v = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
       for (int r = 0; r < RT; ++r) o[r][k] = mfma<BF>(v, p[r], o[r][k]);
@@ -438,6 +468,7 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 2 * RT, 0);
+    __builtin_amdgcn_s_setprio(0);
   };
 #pragma unroll 1
   while (u < u1) {
@@ -489,36 +520,54 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   }
 }
 
-// The splits of a tile joined: a workgroup a row.  A lane takes a split's M and sum,
-// so that their weights are there after one round trip; then the threads of a group
-// (4 channels each) take every GROUPS-th split, B of them in flight.  (With a loop over
-// splits that waits for each, 35 us instead of 8 for 115 rows of four sequences in 64 splits.)
-template <int L, int BF>
+// The splits of a tile joined: a workgroup for 1/PARTS of a row's channels.  A thread
+// takes a split's M and sum, so that their weights are there after one round trip; the
+// threads of a group (4 channels each) take every GROUPS-th split, B of them in
+// flight, the first B before the weights are worked out.  (With a loop over splits
+// that waits for each, 35 us instead of 8 for 115 rows of four sequences in 64.)
+template <int L, int BF, int PARTS>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentAttnArgs a, int rows) {
   constexpr float HEAD = head_of(BF);
-  constexpr int LPR = L / 4, GROUPS = 256 / LPR, B = 8;
-  __shared__ float sm_f[kMostSplits];
+  constexpr int LPR = L / 4 / PARTS, GROUPS = 256 / LPR, B = 8;
+  static_assert(kMostSplits <= 256, "a thread for each split");
+  __shared__ float sm_f[256], sm_m[4], sm_s[4];
   __shared__ __align__(16) float4v sm_v[GROUPS - 1][LPR];
   const int32_t* about = reinterpret_cast<const int32_t*>(a.ws) + kTileWords * blockIdx.x;
   const int splits = about[2];
   if (splits < 2) return;
-  const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.y;
+  const int tid = threadIdx.x, r = blockIdx.y;
   const int64_t step = int64_t(about[1]) * rows * partial_floats(L);
   const float* part = a.ws + kTileWords * kSlots + (int64_t(about[0]) * rows + r) * partial_floats(L);
-  const float* mine = part + min(lane, splits - 1) * step + L;
-  const float m = mine[0], l = lane < splits ? mine[1] : 0.0f;
-  if (mine[2] == 0.0f) return;                            // past the sequence's rows
-  const float M = over_wave(lane < splits ? m : -INFINITY, [](float x, float y) { return fmaxf(x, y); });
+  // of 64 splits at most, every wave works out all of them
+  const int own = splits <= 64 ? tid & 63 : tid;
+  const float* mine = part + min(own, splits - 1) * step + L;
+  const float m = mine[0], ls = mine[1], there = mine[2];
+  const int group = tid / LPR, ch = L / PARTS * int(blockIdx.z) + 4 * (tid % LPR);
+  float4v x[B];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < B; ++k)
+      if (s0 + k * GROUPS < splits) x[k] = *reinterpret_cast<const float4v*>(part + (s0 + k * GROUPS) * step + ch);
+  };
+  load(group);
+  if (there == 0.0f) return;                              // past the sequence's rows
+  // over the splits
+  auto over_all = [&](float v, float* sm, auto f) {
+    v = over_wave(v, f);
+    if (splits <= 64) return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+    if ((tid & 63) == 0) sm[tid >> 6] = v;
+    __syncthreads();
+    return f(f(sm[0], sm[1]), f(sm[2], sm[3]));
+  };
+  const bool valid = own < splits;
+  const float M = over_all(valid ? m : -INFINITY, sm_m, [](float p, float q) { return fmaxf(p, q); });
   const float f = m == -INFINITY ? 1.0f : exp2_fast(m - M);    // nothing seen: zeros, or NaN
-  const float sum = over_wave(l * f, [](float x, float y) { return x + y; });
-  if (tid < kMostSplits) sm_f[lane] = lane < splits ? f : 0.0f;
+  const float sum = over_all(valid ? ls * f : 0.0f, sm_s, [](float p, float q) { return p + q; });
+  sm_f[own] = valid ? f : 0.0f;
   __syncthreads();
-  const int group = tid / LPR, ch = 4 * (tid % LPR);
   float4v v = float4v{0, 0, 0, 0};
   for (int s0 = group; s0 < splits; s0 += GROUPS * B) {
-    float4v x[B];
-#pragma unroll
-    for (int k = 0; k < B; ++k) x[k] = *reinterpret_cast<const float4v*>(part + min(s0 + k * GROUPS, splits - 1) * step + ch);
+    if (s0 != group) load(s0);
 #pragma unroll
     for (int k = 0; k < B; ++k)
       if (s0 + k * GROUPS < splits) v += x[k] * sm_f[s0 + k * GROUPS];
@@ -531,7 +580,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentAttnArgs a, int 
   const int64_t at = int64_t(about[3]) + r;
   v *= sum == 0.0f ? 0.0f : 1.0f / sum;
   *reinterpret_cast<uint2*>(a.out + at * L + ch) = make_uint2(pack2<BF>(v[0], v[1]), pack2<BF>(v[2], v[3]));
-  if (a.lse && tid == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (M - HEAD + __builtin_log2f(sum)) * 0.69314718055994531f;
+  if (a.lse && tid == 0 && blockIdx.z == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (M - HEAD + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 template <int L, int RP, int BF, int RT>
@@ -546,7 +595,11 @@ int launch(LatentAttnArgs a, hipStream_t s) {
   a.target = split ? kSlots : 0;
   const unsigned grid = split ? kSlots : unsigned((tiles + 7) / 8 * 8);
   hipLaunchKernelGGL((latent_attn_kernel<L, RP, BF, RT>), dim3(grid), dim3(256), 0, s, a);
-  if (split) hipLaunchKernelGGL((latent_join_kernel<L, BF>), dim3(unsigned(tiles), ROWS), dim3(256), 0, s, a, ROWS);
+  if (split) {
+    // few rows: a quarter of one to a workgroup
+    if (tiles * ROWS <= 256) hipLaunchKernelGGL((latent_join_kernel<L, BF, 4>), dim3(unsigned(tiles), ROWS, 4), dim3(256), 0, s, a, ROWS);
+    else hipLaunchKernelGGL((latent_join_kernel<L, BF, 1>), dim3(unsigned(tiles), ROWS), dim3(256), 0, s, a, ROWS);
+  }
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
