@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   // 64 bytes further on, but for bit 3), and what it takes for the transposing reads
   const int qat = latent_place<L>(n, g), qat8 = latent_place<L>(n, g + 8) - 128;    // L == 512: the same
   const int vat = latent_place<L>(16 * (g >> 1) + 4 * (g & 1) + (n >> 2), 2 * CT * wave + ((n >> 1) & 1)) + 8 * (n & 1);
-  if (tid < 4) sm_moved[tid] = 0;
+  if (RT == 2 && tid < 4) put_lds(&sm_moved[tid], 0u);     // (the others' are all written in each unit)
 
   auto step = [&](const uint8_t* sm_c, const uint8_t* sm_r, uint8_t* next_c, uint8_t* next_r) __attribute__((always_inline)) {
     meet_loaded();
