@@ -135,6 +135,8 @@ __device__ inline Tile tile_of(const LatentAttnArgs& a, int block, int lane) {
   work = uint32_t(wave_sum(int(work)));
   tiles = wave_sum(tiles);
   int chunk = INT32_MAX / 2;                                   // many tiles: a workgroup each
+  // (a tile that sees nothing has a workgroup too, for its zeros)
+  auto splits_of = [&](int units) { return max(min(int(uint32_t(units + chunk - 1) / uint32_t(chunk)), kMostSplits), 1); };
   if (tiles < a.target) {
     // A split costs its partial's way to memory and back (64 rows of 512 channels 50 ns
     // beside all others', 16 rows 13) where a unit takes a workgroup 2 us: of units u a
@@ -148,14 +150,13 @@ __device__ inline Tile tile_of(const LatentAttnArgs& a, int block, int lane) {
     if (a.r.n_seqs <= 64) {
 #pragma unroll 1
       for (int tries = 0; tries < 4 && !fits; ++tries) {
-        const int made = wave_sum(mine.tiles * min(int(uint32_t(mine.units + chunk - 1) / uint32_t(chunk)), kMostSplits));
+        const int made = wave_sum(mine.tiles * splits_of(mine.units));
         fits = made <= a.target;
         if (!fits) chunk = int(float(chunk) * float(made) / float(a.target)) + 1;
       }
     }
     if (!fits) chunk = even(a.target - tiles);
   }
-  auto splits_of = [&](int units) { return max(min(int(uint32_t(units + chunk - 1) / uint32_t(chunk)), kMostSplits), 1); };
   int made = 0;
   for (int s0 = 0, r = 0; s0 < a.r.n_seqs; s0 += 64) {
     const Share k = s0 ? share(s0, r) : mine;

@@ -38,7 +38,7 @@ def _int32():
     return _torch.int32
 
 
-def _torch_float32():
+def _float32():
     if _torch is None:
         _setup()
     return _torch.float32
@@ -106,6 +106,9 @@ def latent_sizes(cfg: _abi.LatentConfig) -> _abi.PagedSizes:
     return s
 
 
+_NO_QUERIES = (None, 0, 0, None, 0, 0)
+
+
 class _Paged:
     """What the paged caches have in common: their buffers, and the calls on pages.
 
@@ -153,32 +156,30 @@ class _Paged:
         return t.data_ptr(), n - 1
 
     def _rotary(self, freqs, positions, interleaved, n):
-        _need(freqs.dtype == _torch_float32() and freqs.get_device() == self._at and freqs.dim() == 1 and freqs.is_contiguous(),
+        _need(freqs.dtype == _float32() and freqs.get_device() == self._at and freqs.dim() == 1 and freqs.is_contiguous(),
               "freqs: contiguous fp32 of a value for each pair, on %s", self.device)
         return _abi.Rotary(freqs.data_ptr(), None if positions is None else self._ints(positions, "positions", n),
                            2 * freqs.numel(), 1 if interleaved else 0)
 
     def _turned(self, q, q_out, n, heads, dim, dtype):
-        """Addresses and strides of query rows and of their place."""
+        """Where query rows are turned to, and the addresses and strides of both."""
         if q is None:
             _need(q_out is None, "q_out: there is no q")
-            return None, (None, 0, 0, None, 0, 0)
+            return None, _NO_QUERIES
         shape, st = (n, heads, dim), q.stride()
-        _need(q.shape == shape and st[2] == 1 and q.dtype == dtype and q.get_device() == self._at,
+        _need(q.shape == shape and (st[2] == 1 or not n) and q.dtype == dtype and q.get_device() == self._at,
               "q: [%d, %d, %d] of the rows' dtype with a unit channel stride, on %s", n, heads, dim, self.device)
         if q_out is None:
-            import torch
-            q_out = torch.empty(shape, dtype=dtype, device=self.device)
-        else:
-            so = q_out.stride()
-            _need(q_out.shape == shape and so[2] == 1 and q_out.dtype == dtype and q_out.get_device() == self._at,
-                  "q_out: of q's shape and dtype with a unit channel stride")
-            # rows and heads apart from each other, and all of it from q unless it is q
-            _need(so[1] >= dim and so[0] >= heads * so[1] or so[0] >= dim and so[1] >= n * so[0] or n == 1 and so[1] >= dim
-                  or heads == 1 and so[0] >= dim or n * heads <= 1, "q_out: rows that overlap")
-            _need(q_out.data_ptr() == q.data_ptr() and so == st or not _overlap(q, q_out), "q_out: q itself, or apart from q")
-        so = q_out.stride()
-        return q_out, (q.data_ptr(), st[0], st[1], q_out.data_ptr(), so[0], so[1])
+            q_out = q.new_empty(shape)
+            return q_out, (q.data_ptr(), st[0], st[1], q_out.data_ptr(), heads * dim, dim)
+        at, to, so = q.data_ptr(), q_out.data_ptr(), q_out.stride()
+        _need(q_out.shape == shape and so[2] == 1 and q_out.dtype == dtype and q_out.get_device() == self._at,
+              "q_out: of q's shape and dtype with a unit channel stride")
+        # rows and heads apart from each other, and all of it from q unless it is q
+        _need(so[1] >= dim and so[0] >= heads * so[1] or so[0] >= dim and so[1] >= n * so[0] or n == 1 and so[1] >= dim
+              or heads == 1 and so[0] >= dim or n * heads <= 1, "q_out: rows that overlap")
+        _need(to == at and so == st or not _overlap(q, q_out), "q_out: q itself, or apart from q")
+        return q_out, (at, st[0], st[1], to, so[0], so[1])
 
     # -- pages -------------------------------------------------------------
     def assign(self, lens, table):
@@ -346,7 +347,7 @@ class PagedLatent(_Paged):
         return pool
 
     def _part(self, t, what, shape):
-        _need(t.dtype == self.dtype and t.shape == shape and t.stride()[-1] == 1 and t.get_device() == self._at,
+        _need(t.dtype == self.dtype and t.shape == shape and (t.stride()[-1] == 1 or not shape[0]) and t.get_device() == self._at,
               "%s: %s of shape %s with a unit channel stride, on %s", what, self.dtype, shape, self.device)
         return t.stride()
 

@@ -268,6 +268,20 @@ def test_many_sequences(seqs):
     assert cache.status() == 0 and len(lens) == seqs
 
 
+@pytest.mark.parametrize("heads", [16, 64])
+def test_empty_sequences_beside_ones_that_fill_the_chip(heads):
+    """Rows of empty sequences take workgroups too: they come out as zeros, and the others whole."""
+    rng = np.random.default_rng(14)
+    seqs = 64
+    cache = make(heads, 256, 32, "float16", n_pages=8 * 256, seqs=seqs, seq_pages=256)
+    lens = [16384 if s % 8 == 3 else 0 for s in range(seqs)]
+    fill(cache, rng, lens)
+    counts = [1] * seqs
+    q, qr, scale, out, lse = attend(cache, rng, counts)
+    check(cache, q, qr, counts, scale, out, lse, some=[s for s in range(seqs) if s % 8 != 3] + [3, 35, 59])
+    assert out[[s for s in range(seqs) if s % 8 == 3]].abs().sum(-1).all()
+
+
 def test_rows_that_see_nothing():
     """Empty sequences, rows before the first token, missing pages, rows of nobody's."""
     import torch
@@ -349,6 +363,27 @@ def test_in_place_over_the_queries_and_repeats():
         again = cache.attn(0, q, qr, st, 0.05, with_lse=True)
         assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
     assert cache.attn(0, q, qr, st, 0.05, out=q) is q and torch.equal(q, want[0])
+
+
+def test_a_workspace_full_of_rubbish_and_no_rows():
+    import torch
+    rng = np.random.default_rng(15)
+    cache = make(heads=16, latent=512, rope=64, n_pages=80, seq_pages=40)
+    fill(cache, rng, [2000, 10])
+    q, qr = rows(rng, (2, 16, 512), "bfloat16"), rows(rng, (2, 16, 64), "bfloat16")
+    want = cache.attn(0, q, qr, starts_of([1, 1]), 0.05, with_lse=True)
+    for fill_word in (float("nan"), 3.0, -1.0):
+        cache.ws.fill_(fill_word)
+        got = cache.attn(0, q, qr, starts_of([1, 1]), 0.05, with_lse=True)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    cache.ws.view(torch.int32).fill_(7)
+    assert torch.equal(cache.attn(0, q, qr, starts_of([1, 1]), 0.05), want[0])
+    none = cache.attn(0, q[:0], qr[:0], starts_of([0, 0]), 0.05, with_lse=True)
+    assert none[0].shape == (0, 16, 512) and none[1].shape == (0, 16)
+    f = torch.from_numpy(S.frequencies(64)).cuda()
+    kv = rows(rng, (0, 576), "bfloat16")
+    assert cache.append(0, kv[:, :512], kv[:, 512:], starts_of([0, 0]), f, q=qr[:0]).shape == (0, 16, 64)
+    assert cache.status() == 0
 
 
 def test_layers_are_their_own():
