@@ -5,10 +5,17 @@
 // the tiles of both products on v_mfma_f32_16x16x32: a workgroup takes 16 RT rows
 // and a run of the sequence's pages, half a page (a unit of 32 tokens) at a time,
 // which lies in LDS once for both:
-//   scores  C[16 tokens][16 rows] = latents . q        a wave: 16 rows (RT = 4),
-//                                                      or 16 of the tokens
-//   values  C[16 channels][16 rows] = latents^T . p    a wave: a quarter of the
-//                                                      channels, every row
+//   scores  C[16 tokens][16 rows] = latents . q        a wave has 16 rows (64 rows);
+//                                                      16 rows and 16 tokens (32);
+//                                                      16 tokens, half the channels (16)
+//   values  C[16 channels][16 rows] = latents^T . p    a wave has a quarter of the
+//                                                      channels, and every row
+// With 64 rows a wave works out its rows' weights, which cross through LDS.  With
+// fewer the scores do, and every wave works out all weights: its lanes then hold them
+// in the second product's layout, and there is one wait less between the products (one
+// token of 16 heads over 2048: 11.9 us with weights through LDS, 10.8 so; over 32768
+// 21.2 and 19.4; with halves of the channels for 32 rows too, LDS holds one workgroup
+// a CU, and 16 sequences of 16384 tokens with 32 heads take 82 us, not 72).
 // Scores, statistics and sums are fp32; the weights enter the second product in the
 // latents' type (bf16 by 2^-8 of each at most, fp16 2^-11), relative to a running
 // reference M of their row, which is moved only where a unit would pass it by 2^5;
@@ -104,8 +111,9 @@ struct Tile {
 // The units of a call are shared out by what the sequences really hold, so that
 // no more workgroups are made than wanted (a.target; a partial each): a share is
 // the call's tiles times units over the wanted workgroups, at least what makes a
-// split worth its joining, and grows until they suffice.  Where sequences pass 64, or that does not settle, so many are wanted
-// less the tiles: each tile's last share is the only one that is not full.
+// split worth its joining, and grows until they suffice.  Where sequences pass 64, or
+// that does not settle, so many are wanted less the tiles: each tile's last share is
+// the only one that is not full.
 // Consecutive shares of one split go to tiles of the same units: the workgroups
 // of an XCD (every eighth) take consecutive ones, and find each other's units in
 // its L2.
@@ -230,8 +238,8 @@ __device__ inline int weights_place(int row, int group) { return group ^ (row >>
 
 // The second product's operand of latents has channels along lanes and tokens in a
 // lane: 16 lanes read 8 bytes each, four tokens' 16 channels, and get them turned
-// (lane i: channel i of the four tokens).  Lane group g's elements are tokens
-// 16 (g div 2) + 4 (g mod 2) + j, then those + 8.
+// (lane i: channel i of the four tokens).  Lane group g's elements are four tokens in a
+// row, and four further on.
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v lds_short4v;
 __device__ inline uint2 turned4(const uint8_t* p) {
@@ -246,6 +254,9 @@ typedef __attribute__((address_space(3))) void lds_void;
 // have it wait; they go elsewhere.  Counted by meet().
 __device__ inline void put_lds(void* p, uint32_t v) {
   __asm__ volatile("ds_write_b32 %0, %1" : : "v"(uint32_t(uintptr_t((lds_void*)p))), "v"(v) : "memory");
+}
+__device__ inline void put_lds(void* p, float4v v) {
+  __asm__ volatile("ds_write_b128 %0, %1" : : "v"(uint32_t(uintptr_t((lds_void*)p))), "v"(v) : "memory");
 }
 __device__ inline void put_lds(void* p, uint2 v) {
   __asm__ volatile("ds_write_b64 %0, %1" : : "v"(uint32_t(uintptr_t((lds_void*)p))), "v"(uint64_t(v.y) << 32 | v.x) : "memory");
@@ -293,13 +304,16 @@ __device__ __forceinline__ void load_unit(const PagedView& c, int layer, int pag
 
 template <int L, int RP, int BF, int RT>
 __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
-  constexpr int ROWS = 16 * RT, KL = L / 32, KR = RP / 32, CT = L / 64, NQ = RT == 4 ? 2 : 1;   // NQ: token tiles of a wave's scores
+  constexpr int ROWS = 16 * RT, KL = L / 32, KR = RP / 32, CT = L / 64, NQ = RT == 4 ? 2 : 1;   // NQ: tiles of a wave's scores
+  constexpr int KT = KL + KR, PARTS = RT == 1 ? 2 : 1, KH = (KT + PARTS - 1) / PARTS;            // products a score, and a wave's part of them
+  constexpr int RW = RT == 4 ? 1 : RT;                                                           // row tiles that a wave works out weights of
   constexpr float HEAD = head_of(BF);
   __shared__ __align__(64) uint8_t sm_c0[latents_bytes<L>()], sm_c1[latents_bytes<L>()];
   __shared__ __align__(64) uint8_t sm_r0[kUnit * RP * 2], sm_r1[kUnit * RP * 2];
-  __shared__ __align__(16) uint4 sm_p[ROWS][4];
-  __shared__ float sm_max[2][ROWS], sm_alpha[ROWS], sm_l[2][ROWS], sm_m[ROWS];
+  __shared__ __align__(16) uint4 sm_p[RT == 4 ? ROWS : 1][4];
+  __shared__ float sm_alpha[ROWS], sm_l[ROWS], sm_m[ROWS];
   __shared__ __align__(16) uint32_t sm_moved[4];
+  __shared__ __align__(16) float4v sm_x[PARTS][RT == 4 ? 1 : RT][2][RT == 4 ? 1 : 64];           // [part][row tile][token tile][lane]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   const PagedView& c = a.c;
   if (blockIdx.x == gridDim.x - 1)
@@ -310,9 +324,8 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   if (a.target > 0 && tid == 0 && int(blockIdx.x) < a.target && int(blockIdx.x) >= tl.tiles) about[kTileWords * blockIdx.x + 2] = 0;
   if (tl.seq < 0) return;
 
-  // rows of this wave's scores: tile wave mod RT; and its token tile
-  const int rt0 = wave % RT, tt0 = RT == 4 ? 0 : wave / RT;
-  const bool scores = RT == 4 || tt0 < 2;
+  // this wave's scores: of row tile rt0, from token tile tt0 on, part `part` of the channels
+  const int rt0 = wave % RT, tt0 = RT == 4 ? 0 : RT == 2 ? wave >> 1 : wave & 1, part = RT == 1 ? wave >> 1 : 0;
   const int m0 = tl.len - tl.count;
   const int u1 = int(int64_t(tl.units) * (tl.split + 1) / tl.splits);
   // (no kernel writes the table while this one runs: scalar loads)
@@ -334,17 +347,21 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   if (u < u1) load(u, sm_c0, sm_r0);
   int next = find(u + 1);                                 // the unit after u, and in `page` its page
 
-  uint4 q[KL + KR];
-  int limit;                                              // the last token that the lane's row sees
+  uint4 q[KH];
+  int limit[RW];                                          // the last token that the lane's rows see
+#pragma unroll
+  for (int r = 0; r < RW; ++r) limit[r] = m0 + int(uint32_t(min(tl.first + 16 * (RT == 4 ? rt0 : r) + n, tl.rows - 1)) / uint32_t(a.n_heads));
   {
     const int row = min(tl.first + 16 * rt0 + n, tl.rows - 1), i = int(uint32_t(row) / uint32_t(a.n_heads)), h = row - i * a.n_heads;
     const uint16_t* src = a.q + int64_t(tl.row0 + i) * a.qT + h * a.qH + 8 * g;
     const uint16_t* more = a.q_rope + int64_t(tl.row0 + i) * a.rT + h * a.rH + 8 * g;
+    auto queries = [&](auto from) __attribute__((always_inline)) {
+      constexpr int FROM = decltype(from)::value;
 #pragma unroll
-    for (int k = 0; k < KL; ++k) q[k] = *reinterpret_cast<const uint4*>(src + 32 * k);
-#pragma unroll
-    for (int k = 0; k < KR; ++k) q[KL + k] = *reinterpret_cast<const uint4*>(more + 32 * k);
-    limit = m0 + i;
+      for (int k = FROM; k < FROM + KH && k < KT; ++k) q[k - FROM] = *reinterpret_cast<const uint4*>(k < KL ? src + 32 * k : more + 32 * (k - KL));
+    };
+    if (PARTS == 1 || part == 0) queries(std::integral_constant<int, 0>{});
+    else queries(std::integral_constant<int, KH>{});
   }
   const int all_see = m0 + int(uint32_t(tl.first) / uint32_t(a.n_heads));   // what the tile's first row sees, every row does
 
@@ -353,12 +370,46 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int k = 0; k < CT; ++k) o[r][k] = float4v{0, 0, 0, 0};
-  float M = -INFINITY, l = 0.0f;
+  float M[RW], l[RW];
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    M[r] = -INFINITY;
+    l[r] = 0.0f;
+  }
   // places that the lane reads: of its token's chunk g (every fourth further on is
   // 64 bytes further on, but for bit 3), and what it takes for the transposing reads
   const int qat = latent_place<L>(n, g), qat8 = latent_place<L>(n, g + 8) - 128;    // L == 512: the same
-  const int vat = latent_place<L>(16 * (g >> 1) + 4 * (g & 1) + (n >> 2), 2 * CT * wave + ((n >> 1) & 1)) + 8 * (n & 1);
-  if (RT == 2 && tid < 4) put_lds(&sm_moved[tid], 0u);     // (the others' are all written in each unit)
+  const int vt = RT == 4 ? 16 * (g >> 1) + 4 * (g & 1) : 4 * g;             // the operand's first token: those + 8, or + 16, follow
+  const int vat = latent_place<L>(vt + (n >> 2), 2 * CT * wave + ((n >> 1) & 1)) + 8 * (n & 1);
+
+  // a row's weights of 8 of the unit's tokens, from scores x; the factor of the sums so far
+  auto weigh = [&](float (&x)[8], float mx, float& M, float& l, uint4& p) __attribute__((always_inline)) {
+    mx = row_max(mx) * a.scale_log2e;
+    const float Mn = mx > M + kLag || M == -INFINITY ? fmaxf(mx, M) : M;
+    const float alpha = M == -INFINITY || Mn == M ? 1.0f : exp2_fast(M - Mn);
+    M = Mn;
+    l *= alpha;
+    const float ref = M == -INFINITY ? 0.0f : M - HEAD;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = exp2_fast(fmaf(x[e], a.scale_log2e, -ref));
+      l += x[e];
+    }
+    p = make_uint4(pack2<BF>(x[0], x[1]), pack2<BF>(x[2], x[3]), pack2<BF>(x[4], x[5]), pack2<BF>(x[6], x[7]));
+    return alpha;
+  };
+  // scores of tokens 4 g + i and 16 + 4 g + i of unit `at`, without those that the row does not see, and their maximum
+  auto seen_of = [&](float (&x)[8], int at, int limit) __attribute__((always_inline)) {
+    if (at * kUnit + kUnit - 1 > all_see) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at * kUnit + 16 * (e >> 2) + 4 * g + (e & 3) > limit) x[e] = -INFINITY;
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+    return mx;
+  };
 
   auto step = [&](const uint8_t* sm_c, const uint8_t* sm_r, uint8_t* next_c, uint8_t* next_r) __attribute__((always_inline)) {
     meet_loaded();
@@ -367,97 +418,94 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
     const int after = table[min(u + 1, u1 - 1) >> 1];
     if (u < u1) load(u, next_c, next_r);
 
-    float4v x[NQ];
-    float mx = -INFINITY;
-    if (scores) {
+    // two sums for each tile where the tile is the wave's only one: products that wait
+    // for each other take twice as long
+    constexpr int CH = NQ == 1 ? 2 : 1;
+    float4v x[NQ][CH];
+    auto products = [&](auto from) __attribute__((always_inline)) {
+      constexpr int FROM = decltype(from)::value, N = KT - FROM < KH ? KT - FROM : KH;
       __builtin_amdgcn_s_setprio(1);
       const int tile = 16 * tt0;
 #pragma unroll
-      for (int j = 0; j < NQ; ++j) x[j] = float4v{0, 0, 0, 0};
+      for (int k = FROM; k < FROM + N; ++k)
 #pragma unroll
-      for (int k = 0; k < KL; ++k)
-#pragma unroll
-        for (int j = 0; j < NQ; ++j)
-          x[j] = mfma<BF>(*reinterpret_cast<const uint4*>(sm_c + (L == 512 || !(k & 2) ? qat : qat8) + k * 64 + (tile + 16 * j) * (kBlock * L / 512)), q[k], x[j]);
-#pragma unroll
-      for (int k = 0; k < KR; ++k)
-#pragma unroll
-        for (int j = 0; j < NQ; ++j)
-          x[j] = mfma<BF>(*reinterpret_cast<const uint4*>(sm_r + rope_place<RP>(tile + 16 * j + n, 4 * k + g)), q[KL + k], x[j]);
+        for (int j = 0; j < NQ; ++j) {
+          const uint8_t* at = k < KL ? sm_c + (L == 512 || !(k & 2) ? qat : qat8) + k * 64 + (tile + 16 * j) * (kBlock * L / 512)
+                                     : sm_r + rope_place<RP>(tile + 16 * j + n, 4 * (k - KL) + g);
+          const int i = (k - FROM) % CH;
+          x[j][i] = mfma<BF>(*reinterpret_cast<const uint4*>(at), q[k - FROM], k - FROM < CH ? float4v{0, 0, 0, 0} : x[j][i]);
+        }
       // reads a few products ahead
       constexpr int AHEAD = 4 / NQ;
       __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * NQ, 0);
 #pragma unroll
-      for (int k = 0; k < KL + KR - AHEAD; ++k) {
+      for (int k = 0; k < N - AHEAD; ++k) {
         __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, NQ, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * NQ, 0);
       __builtin_amdgcn_s_setprio(0);
-      if (at * kUnit + kUnit - 1 > all_see) {
+    };
+    uint4 p[RT];
+    float alpha[RT];
+    bool moved = false;
+    if constexpr (RT == 4) {
+      products(std::integral_constant<int, 0>{});
+      float y[8] = {x[0][0][0], x[0][0][1], x[0][0][2], x[0][0][3], x[1][0][0], x[1][0][1], x[1][0][2], x[1][0][3]};
+      uint4 w;
+      const float mx = seen_of(y, at, limit[0]), f = weigh(y, mx, M[0], l[0], w);
+      // tokens 4 g + i and 16 + 4 g + i, to where the lanes of the second product take them
 #pragma unroll
-        for (int j = 0; j < NQ; ++j)
+      for (int j = 0; j < 2; ++j)
+        put_lds(reinterpret_cast<uint2*>(&sm_p[16 * rt0 + n][weights_place(n, 2 * j + (g & 1))]) + (g >> 1), j ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y));
+      const bool any = __any(f != 1.0f);                   // rows whose reference has moved
+      if (any && g == 0) put_lds(&sm_alpha[16 * rt0 + n], f);
+      if (lane == 0) put_lds(&sm_moved[rt0], any ? 1u : 0u);
+    } else {
+      if (PARTS == 1 || part == 0) products(std::integral_constant<int, 0>{});
+      else products(std::integral_constant<int, KH>{});
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (at * kUnit + tile + 16 * j + 4 * g + e > limit) x[j][e] = -INFINITY;
-      }
-#pragma unroll
-      for (int j = 0; j < NQ; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[j][e]);
-      mx = row_max(mx) * a.scale_log2e;
-    }
-    if constexpr (RT < 4) {                               // two waves hold a row's tokens
-      if (scores && g == 0) put_lds(&sm_max[tt0][16 * rt0 + n], mx);
-      meet();
-      if (scores) mx = fmaxf(sm_max[0][16 * rt0 + n], sm_max[1][16 * rt0 + n]);
-    }
-    if (scores) {
-      const float Mn = mx > M + kLag || M == -INFINITY ? fmaxf(mx, M) : M;
-      const float alpha = M == -INFINITY || Mn == M ? 1.0f : exp2_fast(M - Mn);
-      M = Mn;
-      l *= alpha;
-      const float ref = M == -INFINITY ? 0.0f : M - HEAD;
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = exp2_fast(fmaf(x[j][e], a.scale_log2e, -ref));
-          l += p[e];
-        }
-        // tokens 16 (tt0 + j) + 4 g + e, in the order of turned4
-        put_lds(reinterpret_cast<uint2*>(&sm_p[16 * rt0 + n][weights_place(n, 2 * (tt0 + j) + (g & 1))]) + (g >> 1),
-                make_uint2(pack2<BF>(p[0], p[1]), pack2<BF>(p[2], p[3])));
-      }
-      if (tt0 == 0) {                                      // rows whose reference has moved
-        const bool moved = __any(alpha != 1.0f);
-        if (moved && g == 0) put_lds(&sm_alpha[16 * rt0 + n], alpha);
-        if (lane == 0) put_lds(&sm_moved[rt0], moved ? 1u : 0u);
-      }
+      for (int j = 0; j < NQ; ++j) put_lds(&sm_x[part][rt0][tt0 + j][lane], CH == 2 ? x[j][0] + x[j][CH - 1] : x[j][0]);
     }
     meet();
     page = after;
     next = u + 1;
     if (page < 0) next = find(u + 1);
-
-    uint4 p[RT];
+    if constexpr (RT == 4) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) p[r] = sm_p[16 * r + n][weights_place(n, g)];
-    const uint4 moved = *reinterpret_cast<const uint4*>(sm_moved);
-    if (__builtin_amdgcn_readfirstlane(RT == 1 ? moved.x : moved.x | moved.y | moved.z | moved.w)) {
-      const uint32_t which[4] = {moved.x, moved.y, moved.z, moved.w};
+      for (int r = 0; r < RT; ++r) p[r] = sm_p[16 * r + n][weights_place(n, g)];
+      const uint4 which = *reinterpret_cast<const uint4*>(sm_moved);
+      moved = __builtin_amdgcn_readfirstlane(which.x | which.y | which.z | which.w);
+      if (moved) {
+        const uint32_t w[4] = {which.x, which.y, which.z, which.w};
+#pragma unroll
+        for (int r = 0; r < RT; ++r) alpha[r] = w[r] ? sm_alpha[16 * r + n] : 1.0f;
+      }
+    } else {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float alpha = which[r] ? sm_alpha[16 * r + n] : 1.0f;
-#pragma unroll
-        for (int k = 0; k < CT; ++k) o[r][k] *= alpha;
+        float4v y0 = sm_x[0][r][0][lane], y1 = sm_x[0][r][1][lane];
+        if constexpr (PARTS == 2) {
+          y0 += sm_x[1][r][0][lane];
+          y1 += sm_x[1][r][1][lane];
+        }
+        float y[8] = {y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
+        const float mx = seen_of(y, at, limit[r]);
+        alpha[r] = weigh(y, mx, M[r], l[r], p[r]);
+        moved = moved || alpha[r] != 1.0f;
       }
+      moved = __any(moved);
+    }
+    if (moved) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int k = 0; k < CT; ++k) o[r][k] *= alpha[r];
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < CT; ++k) {
-      const uint2 lo = turned4(sm_c + vat + 32 * k), hi = turned4(sm_c + vat + 8 * (kBlock * L / 512) + 32 * k);
+      const uint2 lo = turned4(sm_c + vat + 32 * k), hi = turned4(sm_c + vat + (RT == 4 ? 8 : 16) * (kBlock * L / 512) + 32 * k);
       const uint4 v = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
       for (int r = 0; r < RT; ++r) o[r][k] = mfma<BF>(v, p[r], o[r][k]);
@@ -479,15 +527,16 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   }
 
   // the rows' statistics to every wave
-  if (scores) {
-    l = row_sum(l);
+#pragma unroll
+  for (int r = 0; r < RW; ++r) l[r] = row_sum(l[r]);
+  if constexpr (RT == 4) {
     if (g == 0) {
-      sm_l[tt0][16 * rt0 + n] = l;
-      if (tt0 == 0) sm_m[16 * rt0 + n] = M;
+      sm_l[16 * rt0 + n] = l[0];
+      sm_m[16 * rt0 + n] = M[0];
     }
+    __syncthreads();
   }
-  __syncthreads();
-  float* part = a.ws + kTileWords * kSlots + int64_t(tl.slot) * ROWS * partial_floats(L);
+  float* sums = a.ws + kTileWords * kSlots + int64_t(tl.slot) * ROWS * partial_floats(L);
   if (tl.splits > 1 && tl.split == 0 && tid == 0) {
     about[kTileWords * tl.tile] = tl.slot;
     about[kTileWords * tl.tile + 1] = tl.stride;
@@ -498,9 +547,9 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int row = tl.first + 16 * r + n;
-    const float L0 = sm_l[0][16 * r + n] + (RT < 4 ? sm_l[1][16 * r + n] : 0.0f), Mr = sm_m[16 * r + n];
+    const float L0 = RT == 4 ? sm_l[16 * r + n] : l[r % RW], Mr = RT == 4 ? sm_m[16 * r + n] : M[r % RW];
     if (tl.splits > 1) {
-      float* to = part + (16 * r + n) * partial_floats(L);
+      float* to = sums + (16 * r + n) * partial_floats(L);
 #pragma unroll
       for (int k = 0; k < CT; ++k) *reinterpret_cast<float4v*>(to + 16 * (wave * CT + k) + 4 * g) = o[r][k];
       if (wave == 0 && g == 0) {
