@@ -397,6 +397,8 @@ class PagedLatent(_Paged):
         else:
             _need(out.dtype == self.dtype and out.shape == shape and out.is_contiguous() and out.get_device() == self._at,
                   "out: contiguous, of q's shape and dtype")
+            _need((out.data_ptr() == q.data_ptr() and q.is_contiguous() or not _overlap(out, q)) and not _overlap(out, q_rope),
+                  "out: q itself where that is contiguous, or apart from q; apart from q_rope")
         if lse is not None:
             with_lse = True
             _need(lse.dtype == torch.float32 and lse.shape == shape[:2] and lse.is_contiguous()

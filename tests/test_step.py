@@ -213,6 +213,27 @@ def test_binding_of_latents(host):
     assert not rec.calls
 
 
+def test_output_of_latent_attention_beside_its_queries(host):
+    """In place where q is contiguous; an output that meets the queries otherwise is refused."""
+    import torch
+    rec, _, lat = host
+    st = torch.tensor([0, 3, 5], dtype=torch.int32)
+    buf = torch.zeros(2 * 5 * 3 * 576, dtype=torch.float16)
+    q, qr = buf[:5 * 3 * 512].view(5, 3, 512), torch.zeros((5, 3, 64), dtype=torch.float16)
+    assert lat.attn(0, q, qr, st, 0.5, out=q) is q
+    assert rec.calls.pop()[0] == "semkv_latent_attn"
+    both = buf[:5 * 3 * 576].view(5, 3, 576)                              # q and q_rope in one row
+    apart = buf[5 * 3 * 576:][:5 * 3 * 512].view(5, 3, 512)
+    assert lat.attn(0, both[..., :512], both[..., 512:], st, 0.5, out=apart) is apart
+    rec.calls.clear()
+    shifted = buf[512:][:5 * 3 * 512].view(5, 3, 512)
+    for bad in (lambda: lat.attn(0, q, qr, st, 0.5, out=shifted), lambda: lat.attn(0, both[..., :512], both[..., 512:], st, 0.5, out=q),
+                lambda: lat.attn(0, apart, q[..., :64], st, 0.5, out=q)):
+        with pytest.raises(ValueError):
+            bad()
+    assert not rec.calls
+
+
 def test_pool_of_latents_is_checked(abi, monkeypatch):
     import torch
     import paper_2608_28911_amd as M
