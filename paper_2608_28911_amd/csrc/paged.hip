@@ -9,7 +9,9 @@
 // memory-bound from some thousand rows on (8 kv heads, D = G = 128, fp16): 76000
 // rows are written in 88 us (4.5 TB/s of rows in and records out) and read in 75
 // (5.2 TB/s); 15600 of 62000 tokens of 4 layers move in 77 us; one row of each of
-// 16 sequences is written in 3.5 us.
+// 16 sequences is written in 3.5 us.  With 32 query heads beside them and K turned on
+// the way, 76000 rows (D = G = 64) take 186 us (4.4 TB/s), a row of each of 16
+// sequences 4.2.
 #include <type_traits>
 
 #include "paged.h"
