@@ -49,7 +49,10 @@ constexpr int kBufferWord3 = 0x00020000;   // raw buffer of 32-bit elements (gfx
 constexpr float kLag = 5.0f;
 __host__ __device__ constexpr float head_of(bool bf) { return bf ? 0.0f : 10.0f; }
 
-__host__ __device__ constexpr int partial_floats(int latent) { return latent + 4; }   // a row's sums, M and l
+// A partial: sums as the lanes of the second product hold them, [row tile][16
+// channels][lane][4], so that their stores and the join's loads are of 1 KB in a row (by
+// rows 2 us more for 59 MB); then M, sum and whether it is one, of each row.
+__host__ __device__ constexpr int partial_floats(int latent) { return latent + 4; }   // of a row
 
 // The product of 32 channels or tokens.
 template <int BF>
@@ -82,14 +85,6 @@ __device__ inline float over_row(float x, F f) {
 }
 __device__ inline float row_max(float x) { return over_row(x, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ inline float row_sum(float x) { return over_row(x, [](float a, float b) { return a + b; }); }
-
-// Over the wave, in every lane.
-template <class F>
-__device__ inline float over_wave(float x, F f) {
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) x = f(x, __shfl_xor(x, d));
-  return over_row(x, f);
-}
 
 // Sums of the lanes up to each one, by DPP moves: within rows of 16 lanes, then each
 // row's last sum into the next rows.
@@ -556,14 +551,10 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
     const int row = tl.first + 16 * r + n;
     const float L0 = RT == 4 ? sm_l[16 * r + n] : l[r % RW], Mr = RT == 4 ? sm_m[16 * r + n] : M[r % RW];
     if (tl.splits > 1) {
-      float* to = sums + (16 * r + n) * partial_floats(L);
 #pragma unroll
-      for (int k = 0; k < CT; ++k) *reinterpret_cast<float4v*>(to + 16 * (wave * CT + k) + 4 * g) = o[r][k];
-      if (wave == 0 && g == 0) {
-        to[L] = Mr;
-        to[L + 1] = row < tl.rows ? L0 : 0.0f;
-        to[L + 2] = row < tl.rows ? 1.0f : 0.0f;
-      }
+      for (int k = 0; k < CT; ++k) *reinterpret_cast<float4v*>(sums + (r * (L / 16) + wave * CT + k) * 256 + 4 * lane) = o[r][k];
+      if (wave == 0 && g == 0)
+        *reinterpret_cast<float4v*>(sums + ROWS * L + 4 * (16 * r + n)) = row < tl.rows ? float4v{Mr, L0, 1.0f, 0.0f} : float4v{Mr, 0.0f, 0.0f, 0.0f};
     } else if (row < tl.rows) {
       const int64_t at = int64_t(tl.row0) * a.n_heads + row;
       const float f = L0 == 0.0f ? 0.0f : 1.0f / L0;      // no token: zeros
@@ -577,67 +568,81 @@ __global__ __launch_bounds__(256, 2) void latent_attn_kernel(LatentAttnArgs a) {
   }
 }
 
-// The splits of a tile joined: a workgroup for 1/PARTS of a row's channels.  A thread
-// takes a split's M and sum, so that their weights are there after one round trip; the
-// threads of a group (4 channels each) take every GROUPS-th split, B of them in
-// flight, the first B before the weights are worked out.  (With a loop over splits
-// that waits for each, 35 us instead of 8 for 115 rows of four sequences in 64.)
-template <int L, int BF, int PARTS>
-__global__ __launch_bounds__(256) void latent_join_kernel(LatentAttnArgs a, int rows) {
+// The splits of a tile joined: 16 rows by 16 channels are a wave's, or SHARE waves',
+// of which each takes every SHARE-th split.  A thread takes M and sum of some splits of
+// a row, so that their weights are there after one round trip; of the sums B are in
+// flight before these are worked out.  (With a loop over splits that waits for each,
+// 35 us instead of 8 for 115 rows of four sequences in 64.)
+template <int L, int BF, int SHARE>
+__global__ __launch_bounds__(SHARE == 1 ? 256 : 64 * SHARE) void latent_join_kernel(LatentAttnArgs a, int rows) {
   constexpr float HEAD = head_of(BF);
-  constexpr int LPR = L / 4 / PARTS, GROUPS = 256 / LPR, B = 8;
-  static_assert(kMostSplits <= 256, "a thread for each split");
-  __shared__ float sm_f[256], sm_m[4], sm_s[4];
-  __shared__ __align__(16) float4v sm_v[GROUPS - 1][LPR];
+  constexpr int WAVES = SHARE == 1 ? 4 : SHARE, PER = 4 * WAVES, NS = kMostSplits / PER, B = 8;   // PER: splits whose M a pass takes
+  __shared__ float sm_f[kMostSplits][16], sm_m[WAVES][16], sm_s[WAVES][16], sm_there[16];
+  __shared__ __align__(16) float4v sm_v[WAVES - 1][SHARE == 1 ? 1 : 64];
   const int32_t* about = reinterpret_cast<const int32_t*>(a.ws) + kTileWords * blockIdx.x;
   const int splits = about[2];
   if (splits < 2) return;
-  const int tid = threadIdx.x, r = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+  const int t = SHARE == 1 ? 4 * int(blockIdx.z) + wave : int(blockIdx.z), first = SHARE == 1 ? 0 : wave;
   const int64_t step = int64_t(about[1]) * rows * partial_floats(L);
-  const float* part = a.ws + kTileWords * kSlots + (int64_t(about[0]) * rows + r) * partial_floats(L);
-  // of 64 splits at most, every wave works out all of them
-  const int own = splits <= 64 ? tid & 63 : tid;
-  const float* mine = part + min(own, splits - 1) * step + L;
-  const float m = mine[0], ls = mine[1], there = mine[2];
-  const int group = tid / LPR, ch = L / PARTS * int(blockIdx.z) + 4 * (tid % LPR);
+  const float* part = a.ws + kTileWords * kSlots + int64_t(about[0]) * rows * partial_floats(L);
+  const float* stats = part + rows * L + 4 * (16 * int(blockIdx.y) + n);
+  const float* sums = part + (int(blockIdx.y) * (L / 16) + t) * 256 + 4 * lane;
+  const int own = tid >> 4;
+  float4v st[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (PER * i < splits) st[i] = *reinterpret_cast<const float4v*>(stats + min(own + PER * i, splits - 1) * step);
   float4v x[B];
   auto load = [&](int s0) {
 #pragma unroll
     for (int k = 0; k < B; ++k)
-      if (s0 + k * GROUPS < splits) x[k] = *reinterpret_cast<const float4v*>(part + (s0 + k * GROUPS) * step + ch);
+      if (s0 + k * SHARE < splits) x[k] = *reinterpret_cast<const float4v*>(sums + (s0 + k * SHARE) * step);
   };
-  load(group);
-  if (there == 0.0f) return;                              // past the sequence's rows
-  // over the splits
-  auto over_all = [&](float v, float* sm, auto f) {
-    v = over_wave(v, f);
-    if (splits <= 64) return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
-    if ((tid & 63) == 0) sm[tid >> 6] = v;
-    __syncthreads();
-    return f(f(sm[0], sm[1]), f(sm[2], sm[3]));
-  };
-  const bool valid = own < splits;
-  const float M = over_all(valid ? m : -INFINITY, sm_m, [](float p, float q) { return fmaxf(p, q); });
-  const float f = m == -INFINITY ? 1.0f : exp2_fast(m - M);    // nothing seen: zeros, or NaN
-  const float sum = over_all(valid ? ls * f : 0.0f, sm_s, [](float p, float q) { return p + q; });
-  sm_f[own] = valid ? f : 0.0f;
+  load(first);
+  float mx = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (PER * i < splits) mx = fmaxf(mx, st[i][0]);        // (the last split more than once: the same maximum)
+  mx = row_max(mx);
+  if (g == 0) sm_m[wave][n] = mx;
+  if (own == 0) sm_there[n] = st[0][2];
   __syncthreads();
+  float M = sm_m[0][n];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][n]);
+#pragma unroll
+  for (int i = 0; i < NS; ++i)
+    if (own + PER * i < splits) {
+      const float f = st[i][0] == -INFINITY ? 1.0f : exp2_fast(st[i][0] - M);    // nothing seen: zeros, or NaN
+      sm_f[own + PER * i][n] = f;
+      sum += st[i][1] * f;
+    }
+  sum = row_sum(sum);
+  if (g == 0) sm_s[wave][n] = sum;
+  __syncthreads();
+  sum = sm_s[0][n];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) sum += sm_s[w][n];
   float4v v = float4v{0, 0, 0, 0};
-  for (int s0 = group; s0 < splits; s0 += GROUPS * B) {
-    if (s0 != group) load(s0);
+  for (int s0 = first; s0 < splits; s0 += SHARE * B) {
+    if (s0 != first) load(s0);
 #pragma unroll
     for (int k = 0; k < B; ++k)
-      if (s0 + k * GROUPS < splits) v += x[k] * sm_f[s0 + k * GROUPS];
+      if (s0 + k * SHARE < splits) v += x[k] * sm_f[s0 + k * SHARE][n];
   }
-  if (group > 0) sm_v[group - 1][tid % LPR] = v;
-  __syncthreads();
-  if (group > 0) return;
+  if constexpr (SHARE > 1) {
+    if (wave > 0) sm_v[wave - 1][lane] = v;
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-  for (int k = 0; k < GROUPS - 1; ++k) v += sm_v[k][tid];
-  const int64_t at = int64_t(about[3]) + r;
+    for (int k = 0; k < SHARE - 1; ++k) v += sm_v[k][lane];
+  }
+  if (sm_there[n] == 0.0f) return;                         // past the sequence's rows
+  const int64_t at = int64_t(about[3]) + 16 * int(blockIdx.y) + n;
   v *= sum == 0.0f ? 0.0f : 1.0f / sum;
-  *reinterpret_cast<uint2*>(a.out + at * L + ch) = make_uint2(pack2<BF>(v[0], v[1]), pack2<BF>(v[2], v[3]));
-  if (a.lse && tid == 0 && blockIdx.z == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (M - HEAD + __builtin_log2f(sum)) * 0.69314718055994531f;
+  *reinterpret_cast<uint2*>(a.out + at * L + 16 * t + 4 * g) = make_uint2(pack2<BF>(v[0], v[1]), pack2<BF>(v[2], v[3]));
+  if (a.lse && t == 0 && g == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (M - HEAD + __builtin_log2f(sum)) * 0.69314718055994531f;
 }
 
 template <int L, int RP, int BF, int RT>
@@ -653,9 +658,14 @@ int launch(LatentAttnArgs a, hipStream_t s) {
   const unsigned grid = split ? kSlots : unsigned((tiles + 7) / 8 * 8);
   hipLaunchKernelGGL((latent_attn_kernel<L, RP, BF, RT>), dim3(grid), dim3(256), 0, s, a);
   if (split) {
-    // few rows: a quarter of one to a workgroup
-    if (tiles * ROWS <= 256) hipLaunchKernelGGL((latent_join_kernel<L, BF, 4>), dim3(unsigned(tiles), ROWS, 4), dim3(256), 0, s, a, ROWS);
-    else hipLaunchKernelGGL((latent_join_kernel<L, BF, 1>), dim3(unsigned(tiles), ROWS), dim3(256), 0, s, a, ROWS);
+    // blocks of 16 rows by 16 channels: where these are too few for the chip's loads, more
+    // waves share one's splits (one token over 32768, 32 blocks of 128 splits: 21.5 us with
+    // 4 waves, 18.9 with 16; 64 sequences of 2048, 2048 blocks: 33.6 with 4, 32.9 with one,
+    // 44 with 16)
+    const int64_t blocks = tiles * (RT * L / 16);
+    if (blocks <= 128) hipLaunchKernelGGL((latent_join_kernel<L, BF, 16>), dim3(unsigned(tiles), RT, L / 16), dim3(1024), 0, s, a, ROWS);
+    else if (blocks <= 1024) hipLaunchKernelGGL((latent_join_kernel<L, BF, 4>), dim3(unsigned(tiles), RT, L / 16), dim3(256), 0, s, a, ROWS);
+    else hipLaunchKernelGGL((latent_join_kernel<L, BF, 1>), dim3(unsigned(tiles), RT, L / 64), dim3(256), 0, s, a, ROWS);
   }
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
