@@ -4,7 +4,7 @@
 // part that is turned by its position, both kept in 16 bits.  A page holds 64
 // tokens of every layer: [64][latent], then [64][rope].  Both calls move rows and
 // are memory-bound: 28000 rows of 512 + 64 channels and 16 heads' query parts are taken
-// in 44 us (4.1 TB/s in and out), and read back in 12 (from the last-level cache).
+// in 39 us (4.6 TB/s in and out), and read back in 12 (from the last-level cache).
 #include "paged.h"
 #include "rows.h"
 
@@ -28,9 +28,10 @@ __device__ inline bool finite8(const uint4& v) {
 
 constexpr int kParts = 4;        // workgroups that share a page's latents
 constexpr int kQueryHeads = 32;  // query heads of a workgroup
+constexpr int kQueryBlocks = 2048;   // workgroups that queries are shared out to
 
 // The workgroups of a page: kParts for its latents and key parts, a wave a row,
-// then those of the queries.
+// then those of the queries: kQueryHeads heads and a share of the rows each.
 template <int L, int BF>
 __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) {
   constexpr int LANES = L / 8;                             // 16 bytes a lane
@@ -92,9 +93,10 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
     }
     return;
   }
-  // the queries of kQueryHeads heads
-  const int h0 = (int(blockIdx.y) - kParts) * kQueryHeads, heads = min(a.n_heads - h0, kQueryHeads);
-  if (blockIdx.x == 0 && tid < 64) {                       // rows before their sequence's first token: zeros
+  // the queries of kQueryHeads heads, a share of the page's rows
+  const int slice = (int(blockIdx.y) - kParts) / a.q_shares, share = int(blockIdx.y) - kParts - slice * a.q_shares;
+  const int h0 = slice * kQueryHeads, heads = min(a.n_heads - h0, kQueryHeads);
+  if (blockIdx.x == 0 && share == 0 && tid < 64) {                       // rows before their sequence's first token: zeros
     int reached = 0;
     for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
       int len;
@@ -104,8 +106,12 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
           *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + (h0 + j / c.rope) * a.oH + j % c.rope) = make_uint4(0, 0, 0, 0);
     }
   }
-  const PageWork w = page_work(c, a.r, blockIdx.x);
+  PageWork w = page_work(c, a.r, blockIdx.x);
   if (w.seq < 0) return;
+  const int rows = w.hi - w.lo, lo = w.lo;
+  w.hi = lo + rows * (share + 1) / a.q_shares;
+  w.lo = lo + rows * share / a.q_shares;
+  if (w.lo >= w.hi) return;
   make_turns<64>(a.rot, w, turns);
   __syncthreads();
   turn_queries<BF, turns_pitch(64)>(a.rot, w, a.q, a.qT, a.qH, a.q_out, a.oT, a.oH, h0, heads, units, turns);
@@ -153,9 +159,16 @@ static void append_of(const LatentAppendArgs& a, dim3 grid, hipStream_t s) {
   else hipLaunchKernelGGL((latent_append_kernel<L, 0>), grid, dim3(256), 0, s, a);
 }
 
-int launch_latent_append(const LatentAppendArgs& a, hipStream_t s) {
+int launch_latent_append(LatentAppendArgs a, hipStream_t s) {
   const int slices = a.q ? (a.n_heads + kQueryHeads - 1) / kQueryHeads : 0;
-  const dim3 grid(unsigned(touched_bound(a.r)), unsigned(kParts + slices));
+  // the queries' workgroups: a few for each CU where there are few pages, of eight rows at
+  // least (a page's rows to each: 716 rows of 128 heads, with their reading, 23.6 us and
+  // not 15.1; 28000 of 16 heads, 54.7 and not 50.5)
+  const int64_t pages = touched_bound(a.r), rows = a.r.n_rows / pages;
+  int64_t shares = kQueryBlocks / (pages * (slices ? slices : 1));
+  if (shares > rows / 8) shares = rows / 8;
+  a.q_shares = shares < 1 ? 1 : int(shares);
+  const dim3 grid(unsigned(pages), unsigned(kParts + slices * a.q_shares));
   if (a.c.latent == 512) append_of<512>(a, grid, s);
   else append_of<256>(a, grid, s);
   return hipGetLastError() == hipSuccess ? 0 : -5;

@@ -96,7 +96,7 @@ struct LatentAppendArgs {
   RotaryArgs rot;
   const uint16_t* q; uint16_t* q_out;
   int64_t qT, qH, oT, oH;
-  int32_t n_heads, layer, bf16;
+  int32_t n_heads, layer, bf16, q_shares;
 };
 
 struct LatentReadArgs {
@@ -264,7 +264,7 @@ int launch_paged_fork(const PagedView& c, const int32_t* parent, hipStream_t s);
 int launch_paged_compact(const PagedView& c, const int32_t* keep, int64_t ld, const int32_t* n_keep, hipStream_t s);
 int launch_paged_write(PagedWriteArgs a, hipStream_t s);
 int launch_paged_append(PagedAppendArgs a, hipStream_t s);
-int launch_latent_append(const LatentAppendArgs& a, hipStream_t s);
+int launch_latent_append(LatentAppendArgs a, hipStream_t s);
 int launch_latent_read(const LatentReadArgs& a, hipStream_t s);
 size_t latent_attn_workspace(int latent);
 int launch_latent_attn(LatentAttnArgs a, size_t ws_bytes, hipStream_t s);
