@@ -14,7 +14,7 @@
 namespace semkv {
 namespace {
 
-constexpr int kMostKept = 64;                    // candidates of a group (of 64 beams at most)
+constexpr int kMostEach = 4;                     // candidates of a group (64 beams' 64 at most) to a thread that chooses
 
 // Partial of one split of a row: m and pad, S (64 bits), then the kept keys.
 __host__ __device__ constexpr int partial_words(int k) { return 4 + 2 * k; }
@@ -209,11 +209,14 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
 }
 
 // One workgroup chooses a group's candidates: its waves (one for each beam, 16 at
-// most) join the rows' splits, and every kept candidate counts those before it in
-// each row's list, which is in order: its place.
+// most) join the rows' splits, each row's list is in order, and the lists are joined
+// by places: a candidate's is its own in its list and the number of those before it in
+// the other (64 beams of 64: six joins; counting in all 63 other lists at once took 300
+// us).
 __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
   extern __shared__ double sm_t[];                   // [width][k]
   int32_t* sm_v = reinterpret_cast<int32_t*>(sm_t + a.width * a.k);
+  uint16_t* sm_i = reinterpret_cast<uint16_t*>(sm_v + a.width * a.k);
   __shared__ int sm_bad, sm_n;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, threads = blockDim.x;
   const int64_t g = blockIdx.x;
@@ -250,11 +253,14 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
       }
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) S += __shfl_xor(S, d);
-      Kept kept = {0u, 0u};
-      const uint32_t least = kth_order(h, k);        // of the first 64 keys, which the rest cannot lower
-      for (int i = 0; i < a.nsplit * k; i += 64) {
-        if (i) key(i + lane, h, l);
-        keep_all(kept, h != 0 && h >= least, h, l, k, lane);
+      Kept kept = {h, l};                            // one split: its keys are in order
+      if (a.nsplit > 1) {
+        kept = {0u, 0u};
+        const uint32_t least = kth_order(h, k);      // of the first 64 keys, which the rest cannot lower
+        for (int i = 0; i < a.nsplit * k; i += 64) {
+          if (i) key(i + lane, h, l);
+          keep_all(kept, h != 0 && h >= least, h, l, k, lane);
+        }
       }
       // a row without any logit above -inf has no candidates; a NaN or +inf is reported
       const double lse = double(m) + log(S);
@@ -283,31 +289,57 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
     a.tokens[g * k + i] = -1;
   }
   if (bad) return;
-  for (int i = tid; i < a.width * k; i += threads) {
-    const double t = sm_t[i];
-    if (!(t > -INFINITY)) continue;
-    const int mine = i / k;
-    int place = i - mine * k;                        // what is before it in its own list
-    if (a.width * k <= 128) {                        // few: all of them, rather than one read after another
-      place = 0;
+  auto put = [&](int place, double t, int i) {       // candidate i of the lists
+    a.out_scores[g * k + place] = float(t);
+    a.parents[g * k + place] = int32_t(g * a.width + i / k);
+    a.tokens[g * k + place] = sm_v[i];
+  };
+  if (a.width * k <= 128) {                          // few: a candidate counts all that are before it
+    for (int i = tid; i < a.width * k; i += threads) {
+      const double t = sm_t[i];
+      if (!(t > -INFINITY)) continue;
+      int place = 0;
 #pragma unroll 4
       for (int j = 0; j < a.width * k; ++j) place += sm_t[j] > t || (sm_t[j] == t && j < i);
-    } else for (int b = 0; b < a.width && place < k; ++b) {
-      if (b == mine) continue;
-      int lo = 0, hi = k;                            // entries before: larger, or equal and of a lower beam
+      if (place < k) put(place, t, i);
+    }
+    return;
+  }
+  // lists of k in order, joined two by two; equal ones: the lower beams' first
+  for (int i = tid; i < a.width * k; i += threads) sm_i[i] = uint16_t(i);
+  __syncthreads();
+  for (int s = 1; s < a.width; s <<= 1) {
+    const int pairs = (a.width + s - 1) / (2 * s);   // of lists 2 p s and 2 p s + s
+    double t[kMostEach];
+    int i[kMostEach], to[kMostEach];
+#pragma unroll
+    for (int e = 0; e < kMostEach; ++e) {
+      const int at = tid + e * threads;
+      to[e] = -1;
+      if (at >= pairs * 2 * k) continue;
+      const int pair = int(uint32_t(at) / uint32_t(2 * k)), r = at - pair * 2 * k, upper = r >= k, j = r - upper * k;
+      const int own = (2 * pair + upper) * s * k, other = (2 * pair + 1 - upper) * s * k;
+      t[e] = sm_t[own + j];
+      i[e] = sm_i[own + j];
+      int lo = 0, hi = k - j;                        // entries of the other list before it; at k places it is out
       while (lo < hi) {
         const int mid = (lo + hi) / 2;
-        const double u = sm_t[b * k + mid];
-        if (u > t || (u == t && b < mine)) lo = mid + 1;
+        const double u = sm_t[other + mid];
+        if (u > t[e] || (u == t[e] && upper)) lo = mid + 1;
         else hi = mid;
       }
-      place += lo;
+      if (j + lo < k) to[e] = 2 * pair * s * k + j + lo;
     }
-    if (place >= k) continue;
-    a.out_scores[g * k + place] = float(t);
-    a.parents[g * k + place] = int32_t(g * a.width + mine);
-    a.tokens[g * k + place] = sm_v[i];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kMostEach; ++e)
+      if (to[e] >= 0) {
+        sm_t[to[e]] = t[e];
+        sm_i[to[e]] = uint16_t(i[e]);
+      }
+    __syncthreads();
   }
+  if (tid < k && sm_t[tid] > -INFINITY) put(tid, sm_t[tid], sm_i[tid]);
 }
 
 // Splits of a row: enough workgroups for the chip where there are few rows, each
@@ -334,7 +366,7 @@ int launch_beam_select(BeamArgs a, hipStream_t s) {
   else if (a.dtype == 1) hipLaunchKernelGGL((beam_rows_kernel<1, 4>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((beam_rows_kernel<2, 4>), grid, dim3(256), 0, s, a);
   const int waves = a.width < 16 ? a.width : 16;
-  hipLaunchKernelGGL(beam_choose_kernel, dim3(unsigned(a.groups)), dim3(64 * waves), size_t(a.width) * a.k * 12, s, a);
+  hipLaunchKernelGGL(beam_choose_kernel, dim3(unsigned(a.groups)), dim3(64 * waves), size_t(a.width) * a.k * 14, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
