@@ -16,6 +16,8 @@ namespace {
 
 constexpr int kMostEach = 4;                     // candidates of a group (64 beams' 64 at most) to a thread that chooses
 
+constexpr int kAtOnce = 8, kSure = 120;          // keys of a row's splits that a lane takes at once; those that a wave counts into order
+
 // Partial of one split of a row: m and pad, S (64 bits), then the kept keys.
 __host__ __device__ constexpr int partial_words(int k) { return 4 + 2 * k; }
 
@@ -208,15 +210,23 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   }
 }
 
+// LDS accesses of the wave's other lanes before what follows.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // One workgroup chooses a group's candidates: its waves (one for each beam, 16 at
 // most) join the rows' splits, each row's list is in order, and the lists are joined
 // by places: a candidate's is its own in its list and the number of those before it in
 // the other (64 beams of 64: six joins; counting in all 63 other lists at once took 300
 // us).
+template <bool MANY>
 __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
   extern __shared__ double sm_t[];                   // [width][k]
-  int32_t* sm_v = reinterpret_cast<int32_t*>(sm_t + a.width * a.k);
-  uint16_t* sm_i = reinterpret_cast<uint16_t*>(sm_v + a.width * a.k);
+  uint2* sm_sure = reinterpret_cast<uint2*>(sm_t + a.width * a.k);         // [waves][kSure], and later
+  uint16_t* sm_i = reinterpret_cast<uint16_t*>(sm_sure);                   // [width][k]: no more than 256 a wave
+  int32_t* sm_v = reinterpret_cast<int32_t*>(sm_sure + (blockDim.x >> 6) * kSure);   // [width][k]
   __shared__ int sm_bad, sm_n;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = a.k, threads = blockDim.x;
   const int64_t g = blockIdx.x;
@@ -241,8 +251,14 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
         l = q[1];
         if (!valid) h = l = 0;
       };
-      uint32_t h, l;
-      key(lane, h, l);
+      const int total = a.nsplit * k;
+      constexpr int N = MANY ? kAtOnce : 1;
+      uint32_t h[N], l[N];
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        h[c] = l[c] = 0;
+        if (64 * c < total) key(64 * c + lane, h[c], l[c]);
+      }
       float m = kFloor;
       for (int i = lane; i < a.nsplit; i += 64) m = fmaxf(m, __uint_as_float(p[i * partial_words(k)]));
       m = over_wave(m, [](float x, float y) { return fmaxf(x, y); });
@@ -253,13 +269,66 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
       }
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) S += __shfl_xor(S, d);
-      Kept kept = {h, l};                            // one split: its keys are in order
-      if (a.nsplit > 1) {
+      Kept kept = {h[0], l[0]};                      // one split: its keys are in order
+      if (!MANY && a.nsplit > 1) {
         kept = {0u, 0u};
-        const uint32_t least = kth_order(h, k);      // of the first 64 keys, which the rest cannot lower
-        for (int i = 0; i < a.nsplit * k; i += 64) {
-          if (i) key(i + lane, h, l);
-          keep_all(kept, h != 0 && h >= least, h, l, k, lane);
+        const uint32_t least = kth_order(h[0], k);   // of the first 64 keys, which the rest cannot lower
+        for (int i = 0; i < total; i += 64) {
+          if (i) key(i + lane, h[0], l[0]);
+          keep_all(kept, h[0] != 0 && h[0] >= least, h[0], l[0], k, lane);
+        }
+      }
+      if (MANY) {
+        // keys that reach the k-th largest of the first ones are counted into order; where
+        // ties are more than there is room for, a list is kept
+        uint32_t least = 0;
+#pragma unroll
+        for (int b = 31; b >= 16; --b) {
+          int n = 0;
+#pragma unroll
+          for (int c = 0; c < N; ++c) n += __popcll(__ballot(h[c] >= (least | 1u << b)));
+          if (n >= k) least |= 1u << b;
+        }
+        uint2* sure = sm_sure + wave * kSure;
+        int n = 0;
+        auto take = [&](uint32_t h, uint32_t l) {
+          const bool may = h != 0 && h >= least;
+          const uint64_t who = __ballot(may);
+          const int at = n + int(__builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0)));
+          if (may && at < kSure) sure[at] = make_uint2(h, l);
+          n += __popcll(who);
+        };
+#pragma unroll
+        for (int c = 0; c < N; ++c) take(h[c], l[c]);
+        for (int i = 64 * N; i < total; i += 64) {
+          uint32_t hi, lo;
+          key(i + lane, hi, lo);
+          take(hi, lo);
+        }
+        if (n <= kSure) {
+          wave_sync();
+          const uint2 x = sure[min(lane, kSure - 1)], y = sure[min(64 + lane, kSure - 1)];
+          int px = 0, py = 0;
+#pragma unroll 4
+          for (int i = 0; i < n; ++i) {
+            const uint2 z = sure[i];
+            px += z.x > x.x || (z.x == x.x && z.y > x.y);
+            py += z.x > y.x || (z.x == y.x && z.y > y.y);
+          }
+          wave_sync();
+          if (lane < n) sure[px] = x;
+          if (64 + lane < n) sure[py] = y;
+          wave_sync();
+          const uint2 z = sure[lane];
+          kept = lane < n ? Kept{z.x, z.y} : Kept{0u, 0u};
+          wave_sync();                               // (the wave's next beam)
+        } else {
+          kept = {0u, 0u};
+          for (int i = 0; i < total; i += 64) {
+            uint32_t hi, lo;
+            key(i + lane, hi, lo);
+            keep_all(kept, hi != 0 && hi >= least, hi, lo, k, lane);
+          }
         }
       }
       // a row without any logit above -inf has no candidates; a NaN or +inf is reported
@@ -366,7 +435,12 @@ int launch_beam_select(BeamArgs a, hipStream_t s) {
   else if (a.dtype == 1) hipLaunchKernelGGL((beam_rows_kernel<1, 4>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((beam_rows_kernel<2, 4>), grid, dim3(256), 0, s, a);
   const int waves = a.width < 16 ? a.width : 16;
-  hipLaunchKernelGGL(beam_choose_kernel, dim3(unsigned(a.groups)), dim3(64 * waves), size_t(a.width) * a.k * 14, s, a);
+  const size_t lds = size_t(a.width) * a.k * 12 + size_t(waves) * kSure * 8;
+  // many keys of a row's splits are counted, few put into a list one after another (8 beams'
+  // 32 best, 384 keys each: 40 us a call in a list, 28 counted; 4 beams' 4 best, 60 keys:
+  // 11.7 and 14.2)
+  if (a.nsplit * a.k > 128) hipLaunchKernelGGL((beam_choose_kernel<true>), dim3(unsigned(a.groups)), dim3(64 * waves), lds, s, a);
+  else hipLaunchKernelGGL((beam_choose_kernel<false>), dim3(unsigned(a.groups)), dim3(64 * waves), lds, s, a);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 

@@ -91,6 +91,34 @@ def test_ties_go_to_the_lower_beam_and_token(dtype, V):
     check(torch.zeros((1, 3, V), dtype=x.dtype, device="cuda"), [[0.0, 0.0, 0.0]], 5)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("G,W,V,k", [(1, 64, 20001, 64), (1, 2, 131073, 64), (2, 17, 17000, 40), (1, 7, 70000, 33),
+                                    (1, 33, 40000, 5), (3, 3, 90000, 50)])
+def test_many_candidates(dtype, G, W, V, k):
+    """Lists of many beams, of many splits, of both; widths that are no powers of two; beams not in use, and ended ones."""
+    rng = np.random.default_rng(W * k)
+    x = logits_of(rng, (G, W, V), dtype)
+    scores = -4 - 2 * rng.random((G, W)).astype(np.float32)
+    check(x, scores, k)
+    ended = (rng.random((G, W)) < 0.3).astype(np.int32)
+    scores[rng.random((G, W)) < 0.3] = -np.inf
+    check(x, scores, k, ended, pad=9)
+
+
+@pytest.mark.parametrize("every", [1, 7, 1400, 2800])
+def test_many_ties(every):
+    """The k-th largest of 64 ties with all, with a seventh, or with some 100 or 50 of 140000 logits: a few more than k, or
+    more than there is room to count."""
+    import torch
+    x = torch.full((1, 3, 140000), -2.0, device="cuda")
+    x[..., 5::every] = 1.5
+    x[0, 1, 139000:139010] = 2.0
+    got = check(x, [[-1.0, -1.0, -1.0]], 64)
+    assert list(got[1][0][:10]) == [1] * 10 and list(got[2][0][:10]) == list(range(139000, 139010))
+    check(x[:, :1], [[-1.0]], 64)
+    check(x[:, :, :20000].expand(1, 3, 20000), [[-1.0, -1.0, -1.5]], 60)
+
+
 def test_first_step_ended_beams_and_empty_rows():
     rng = np.random.default_rng(5)
     x = logits_of(rng, (4, 4, 700), "float16")
