@@ -22,8 +22,8 @@
 // fp16 weights are 2^10 at the reference, so that they keep their bits down to 2^-24
 // of it.
 //
-// 512 tokens of 16 heads over 16384 take 283 us (1.05 PFLOP/s): LDS is busy 42 % of
-// the time by address and some 20 more under loads, beside matrix cores at 50 %.  16
+// 512 tokens of 16 heads over 16384 take 281 us (1.06 PFLOP/s): LDS is busy 43 % of
+// the time by address and some 20 more under loads, beside matrix cores at 51 %.  16
 // single tokens over up to 16384 read at 4.2 TB/s (55 us a call, on states in turn).
 // 128 heads of 8 sequences over 16384, 64 us, and five tokens of 4 over 32768, 41, have
 // 20 us that do not grow with the tokens: the splits' partials go to memory and back

@@ -691,8 +691,8 @@ __device__ inline void early_queries(const PagedAppendArgs& a) {
 }
 
 // Write with the rotation on the way.  The workgroups of a page: for each kv head
-// its K, turned before it is quantized, and its V, as above; and as many for the
-// queries, each a share of the page's rows with every head, which lie together in
+// its K, turned before it is quantized, and its V, as above; and as many or more for
+// the queries, each a share of the page's rows with every head, which lie together in
 // memory and turn alike (a share of the heads with every row instead: 217 us for
 // 76000 rows of 8 kv heads and 32 query heads of 64 channels, not 186).  Of those 186
 // us 63 are K's and V's (written without a turn 42), the rest the queries' (a copy of
