@@ -235,35 +235,42 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
   for (int b = wave; b < a.width; b += threads >> 6) {
     const int64_t row = g * a.width + b;
     const float score = a.scores[row];
+    const int ended = a.ended ? a.ended[row] : 0;
+    // all of these are under way before the first is looked at (what is not read of a
+    // row that has no candidates is not used)
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(a.ws) + row * a.nsplit * partial_words(k);
+    const int total = a.nsplit * k;
+    auto key = [&](int at, uint32_t& h, uint32_t& l) {
+      const int sp = at / k, j = at - sp * k;
+      const bool valid = at < total;
+      const uint32_t* q = p + (valid ? sp * partial_words(k) + 4 + 2 * j : 0);
+      h = q[0];
+      l = q[1];
+      if (!valid) h = l = 0;
+    };
+    constexpr int N = MANY ? kAtOnce : 1;
+    uint32_t h[N], l[N];
+    const uint32_t* own = p + min(lane, a.nsplit - 1) * partial_words(k);
+    const float own_m = lane < a.nsplit ? __uint_as_float(own[0]) : kFloor;
+    const double own_S = *reinterpret_cast<const double*>(own + 2);
+    key(lane, h[0], l[0]);
     double t = -INFINITY;
     int32_t v = 0;
     bool bad = !(score < INFINITY);
-    if (a.ended && a.ended[row]) {
+    if (ended) {
       if (lane == 0) t = double(score);
       v = a.pad;
     } else if (score != -INFINITY) {
-      const uint32_t* p = reinterpret_cast<const uint32_t*>(a.ws) + row * a.nsplit * partial_words(k);
-      auto key = [&](int at, uint32_t& h, uint32_t& l) {
-        const int sp = at / k, j = at - sp * k;
-        const bool valid = at < a.nsplit * k;
-        const uint32_t* q = p + (valid ? sp * partial_words(k) + 4 + 2 * j : 0);
-        h = q[0];
-        l = q[1];
-        if (!valid) h = l = 0;
-      };
-      const int total = a.nsplit * k;
-      constexpr int N = MANY ? kAtOnce : 1;
-      uint32_t h[N], l[N];
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
+      for (int c = 1; c < N; ++c) {
         h[c] = l[c] = 0;
         if (64 * c < total) key(64 * c + lane, h[c], l[c]);
       }
-      float m = kFloor;
-      for (int i = lane; i < a.nsplit; i += 64) m = fmaxf(m, __uint_as_float(p[i * partial_words(k)]));
+      float m = own_m;
+      for (int i = lane + 64; i < a.nsplit; i += 64) m = fmaxf(m, __uint_as_float(p[i * partial_words(k)]));
       m = over_wave(m, [](float x, float y) { return fmaxf(x, y); });
-      double S = 0.0;
-      for (int i = lane; i < a.nsplit; i += 64) {
+      double S = lane < a.nsplit ? own_S * double(exp_of(own_m - m)) : 0.0;
+      for (int i = lane + 64; i < a.nsplit; i += 64) {
         const uint32_t* q = p + i * partial_words(k);
         S += *reinterpret_cast<const double*>(q + 2) * double(exp_of(__uint_as_float(q[0]) - m));
       }
