@@ -28,11 +28,6 @@ __device__ inline void raise(Row& a, float m) {   // m >= a.m
   a.m = m;
 }
 
-// A beam that has candidates of its own row.
-__device__ inline bool reads_row(const BeamArgs& a, int64_t row) {
-  return a.scores[row] != -INFINITY && !(a.ended && a.ended[row]);
-}
-
 // 16 bytes from an element's address (global loads need no more on gfx950).
 template <int DT>
 __device__ inline uint4 load_anywhere(const char* p) {
@@ -57,12 +52,17 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   __shared__ int sm_n[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
+  const float score = a.scores[row];
+  const int ended = a.ended ? a.ended[row] : 0;
   const int64_t g = row / a.width;
   const char* x = static_cast<const char*>(a.x) + (g * a.s_group + (row - g * a.width) * a.s_beam) * Elem<DT>::size;
   // vectors from the row's first element on, wherever that lies: rows of the same
   // logits have the same sum to the last bit, and their candidates stay equal
   const int64_t vecs = a.vocab / V;
   const int64_t v0 = vecs * blockIdx.y / a.nsplit, v1 = vecs * (blockIdx.y + 1) / a.nsplit;
+  // a beam that has no candidates of its own row may have no logits in memory: looked at
+  // before the first load (the places above are worked out meanwhile)
+  if (score == -INFINITY || ended) return;
   Row s = {kFloor, 0.0f};
   const int k = a.k;
 
@@ -80,7 +80,6 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
     }
   };
   load(v0 + tid);
-  if (!reads_row(a, row)) return;                            // (looked at while the first logits come)
   for (int64_t v = v0 + tid; v < v1; v += NT * U) {
     uint4 w[U];
 #pragma unroll
