@@ -568,8 +568,11 @@ int semkv_latent_attn(const semkv_latent* c, int32_t layer, const void* q, int64
  * [groups][width] rows of `vocab` (dtype F16, BF16 or F32; element (g, b, i) at
  * g*s_group + b*s_beam + i), the k candidates of the largest
  *   t(b, i) = a_b + x_b[i] - ln sum_u exp(x_b[u]),
- * in descending order, equal ones by lower beam, then lower token (rows' sums are
- * joined, and t is worked out and compared, in 64 bits):
+ * in descending order, equal ones by lower beam, then lower token.  A row's sum is
+ * kept, and t worked out and compared, in 64 bits; the exponentials are fp32: ln sum is
+ * off by (2.3 ln vocab + 5) 2^-24 at most (2e-6), about 2e-8 as a rule, and candidates
+ * of different beams that are closer than that may come in either order (rows of the
+ * same logits have the same sum to the last bit):
  *   out_scores fp32 [groups][k]: t, rounded
  *   parents int32 [groups][k]:   g * width + b: the slot, as semkv_paged_fork takes it
  *   tokens int32 [groups][k]:    i

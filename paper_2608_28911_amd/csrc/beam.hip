@@ -5,9 +5,14 @@
 //
 // Within a row t follows x, so one pass over the logits keeps a row's k largest by
 // (x, v) and its sum of exponentials, and candidates of different rows meet only
-// afterwards, k of each.  There the order can hang on the last place: rows' sums
-// are joined, their logarithm is taken and t is worked out in 64 bits (a lane's
-// own sums are fp32, a vector of logits at a time: 2e-8 of ln sum in all).
+// afterwards, k of each.  There the order can hang on the last place: a lane's sums
+// are kept, joined and scaled, their logarithm is taken and t is worked out in 64 bits.
+// What is fp32 are the exponentials and the sum of a vector's: (2.23 ln V + 5) 2^-24 of
+// ln sum at most (e^-y is off by its argument's roundings, 2.23 y 2^-24, and a step of
+// the power of two; y, which the exponentials weigh, is no more than the row's entropy
+// on average; three additions), 2e-6 for 160000 logits, 2e-8 where roundings go either
+// way.  (With a lane's sums in fp32 it grows with V: 7e-6 where many small exponentials
+// stand beside a large one.)
 #include "paged.h"
 #include "tokens.h"
 
@@ -21,11 +26,55 @@ constexpr int kAtOnce = 8, kSure = 120;          // keys of a row's splits that 
 // Partial of one split of a row: m and pad, S (64 bits), then the kept keys.
 __host__ __device__ constexpr int partial_words(int k) { return 4 + 2 * k; }
 
-struct Row { float m, S; };                       // a lane's maximum, and sum e^(x-m)
+// e^d for d <= 0 (sums below a larger maximum), to 4e-13: 2^k times the series of what
+// is left, |r| <= ln 2 / 2, as far as r^10/10!.  (Every wave comes by here: with exp()
+// 0.3 to 1.1 us a call more.)
+__device__ inline double exp_below(double d) {
+  d = fmax(d, -1000.0);                           // 0 from there on
+  const double k = rint(d * 1.4426950408889634), r = fma(k, -0.6931471805599453, d);
+  double e = 1.0 / 3628800;
+  e = fma(e, r, 1.0 / 362880);
+  e = fma(e, r, 1.0 / 40320);
+  e = fma(e, r, 1.0 / 5040);
+  e = fma(e, r, 1.0 / 720);
+  e = fma(e, r, 1.0 / 120);
+  e = fma(e, r, 1.0 / 24);
+  e = fma(e, r, 1.0 / 6);
+  e = fma(e, r, 0.5);
+  e = fma(e, r, 1.0);
+  e = fma(e, r, 1.0);
+  return ldexp(e, int(k));
+}
+
+struct Row { float m; double S; };                // a lane's maximum, and sum e^(x-m)
 
 __device__ inline void raise(Row& a, float m) {   // m >= a.m
-  a.S *= exp_of(a.m - m);
+  a.S *= exp_below(double(a.m) - double(m));
   a.m = m;
+}
+
+// The lanes' sum, in every lane, as over_wave.
+__device__ inline double sum_wave(double x) {
+  auto with = [](double v, auto move) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = move(uint32_t(u)), hi = move(uint32_t(u >> 32));
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+  };
+  auto dpp = [](auto ctrl) {
+    return [](uint32_t v) { return uint32_t(__builtin_amdgcn_mov_dpp(int(v), decltype(ctrl)::value, 0xF, 0xF, true)); };
+  };
+  x += with(x, dpp(std::integral_constant<int, 0xB1>{}));    // lane xor 1
+  x += with(x, dpp(std::integral_constant<int, 0x4E>{}));    // lane xor 2
+  x += with(x, dpp(std::integral_constant<int, 0x141>{}));   // mirror of 8 lanes
+  x += with(x, dpp(std::integral_constant<int, 0x140>{}));   // mirror of 16
+  // rows of 16 lanes, and halves of the wave, are exchanged
+  auto pair = [](double v, auto swap) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const auto lo = swap(uint32_t(u)), hi = swap(uint32_t(u >> 32));
+    return __builtin_bit_cast(double, uint64_t(hi[0]) << 32 | lo[0]) + __builtin_bit_cast(double, uint64_t(hi[1]) << 32 | lo[1]);
+  };
+  x = pair(x, [](uint32_t v) { return __builtin_amdgcn_permlane16_swap(v, v, false, false); });
+  return pair(x, [](uint32_t v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); });
 }
 
 // 16 bytes from an element's address (global loads need no more on gfx950).
@@ -46,7 +95,7 @@ __device__ inline uint4 load_anywhere(const char* p) {
 template <int DT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   constexpr int V = Elem<DT>::vec, NT = 64 * WAVES, U = 4;
-  __shared__ Row sm[WAVES];
+  __shared__ double sm_S[WAVES];
   __shared__ uint32_t sm_most[NT];
   __shared__ uint32_t sm_hi[NT], sm_lo[NT];                  // a wave's candidates: 64 of them
   __shared__ int sm_n[WAVES];
@@ -63,7 +112,7 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   // a beam that has no candidates of its own row may have no logits in memory: looked at
   // before the first load (the places above are worked out meanwhile)
   if (score == -INFINITY || ended) return;
-  Row s = {kFloor, 0.0f};
+  Row s = {kFloor, 0.0};
   const int k = a.k;
 
   // what is behind the last whole vector
@@ -79,32 +128,47 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
       if (at < v1) next[u] = load_anywhere<DT>(x + 16 * at);
     }
   };
+  // `count` vectors to the sum: the maximum of all, then each one's exponentials (in some
+  // lane of a wave the maximum rises nearly every time, which is 20 instructions in 64
+  // bits: with a vector at a time 256 rows of 128000 take 2.3 us more)
+  auto sum = [&](auto count, const uint4* w) __attribute__((always_inline)) {
+    constexpr int N = decltype(count)::value;
+    float e[N][V], mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      unpack<DT>(w[u], e[u]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) mx = fmaxf(mx, e[u][i]);
+    }
+    if (mx > s.m) raise(s, mx);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      float p[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = exp_of(e[u][i] - s.m);
+#pragma unroll
+      for (int d = V / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int i = 0; i < d; ++i) p[i] += p[i + d];
+      s.S += double(p[0]);
+    }
+  };
   load(v0 + tid);
   for (int64_t v = v0 + tid; v < v1; v += NT * U) {
     uint4 w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) w[u] = next[u];
     load(v + NT * U);                                        // under way while these are looked at
+    if (v + NT * (U - 1) < v1) {
+      sum(std::integral_constant<int, U>{}, w);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (v + u * NT >= v1) break;
-      float e[V], p[V];
-      unpack<DT>(w[u], e);
-      float mx = e[0];
-#pragma unroll
-      for (int i = 1; i < V; ++i) mx = fmaxf(mx, e[i]);
-      if (mx > s.m) raise(s, mx);
-#pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = exp_of(e[i] - s.m);
-#pragma unroll
-      for (int d = V / 2; d > 0; d /= 2)
-#pragma unroll
-        for (int i = 0; i < d; ++i) p[i] += p[i + d];
-      s.S += p[0];
+      for (int u = 0; u < U - 1; ++u)
+        if (v + u * NT < v1) sum(std::integral_constant<int, 1>{}, w + u);
     }
   }
   if (last > s.m) raise(s, last);
-  s.S += ends ? exp_of(last - s.m) : 0.0f;
+  s.S += ends ? double(exp_of(last - s.m)) : 0.0;
 
   // the bound: of the lanes' largest, in the order of their upper 16 bits
   sm_most[tid] = order_of(s.m);
@@ -112,6 +176,15 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   uint32_t most[WAVES], least = 0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) most[w] = sm_most[64 * w + lane];
+  // the lanes' sums relative to the workgroup's maximum
+  float m = logit_of(most[0]);
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, logit_of(most[w]));
+  m = over_wave(m, [](float p, float q) { return fmaxf(p, q); });
+  const float own = s.m;
+  raise(s, m);
+  const double S = sum_wave(s.S);
+  if (lane == 0) sm_S[wave] = S;
 #pragma unroll
   for (int b = 31; b >= 16; --b) {
     int n = 0;
@@ -122,7 +195,7 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   const float bound = least > order_of(-INFINITY) ? logit_of(least) : kFloor;   // -inf is no candidate
   // f(may, order, complemented index): every logit of this wave that reaches the bound
   auto visit = [&](auto f) {
-    uint64_t who = __ballot(s.m >= bound);
+    uint64_t who = __ballot(own >= bound);
     while (who) {                                            // four lanes' vectors at a time
       constexpr int B = 4;
       int from[B];
@@ -173,12 +246,6 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
     n = k;
   }
   if (lane == 0) sm_n[wave] = n;
-
-  // the lanes' sums relative to the wave's maximum
-  auto add = [](float p, float q) { return p + q; };
-  raise(s, over_wave(s.m, [](float p, float q) { return fmaxf(p, q); }));
-  s.S = over_wave(s.S, add);
-  if (lane == 0) sm[wave] = s;
   __syncthreads();
   // every candidate counts those before it: its place
   uint32_t* p = reinterpret_cast<uint32_t*>(a.ws) + (row * a.nsplit + blockIdx.y) * partial_words(k);
@@ -198,14 +265,11 @@ __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   }
   for (int i = all + tid; i < k; i += NT) p[4 + 2 * i] = p[5 + 2 * i] = 0;
   if (tid == 0) {
-    float m = sm[0].m;
+    double all = sm_S[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w].m);
-    double S = 0.0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) S += double(sm[w].S) * double(exp_of(sm[w].m - m));
+    for (int w = 1; w < WAVES; ++w) all += sm_S[w];
     p[0] = __float_as_uint(m);
-    *reinterpret_cast<double*>(p + 2) = S;
+    *reinterpret_cast<double*>(p + 2) = all;
   }
 }
 
@@ -268,10 +332,10 @@ __global__ __launch_bounds__(1024) void beam_choose_kernel(BeamArgs a) {
       float m = own_m;
       for (int i = lane + 64; i < a.nsplit; i += 64) m = fmaxf(m, __uint_as_float(p[i * partial_words(k)]));
       m = over_wave(m, [](float x, float y) { return fmaxf(x, y); });
-      double S = lane < a.nsplit ? own_S * double(exp_of(own_m - m)) : 0.0;
+      double S = lane < a.nsplit ? own_S * exp_below(double(own_m) - double(m)) : 0.0;
       for (int i = lane + 64; i < a.nsplit; i += 64) {
         const uint32_t* q = p + i * partial_words(k);
-        S += *reinterpret_cast<const double*>(q + 2) * double(exp_of(__uint_as_float(q[0]) - m));
+        S += *reinterpret_cast<const double*>(q + 2) * exp_below(double(__uint_as_float(q[0])) - double(m));
       }
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) S += __shfl_xor(S, d);
