@@ -96,18 +96,14 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
   // the queries of kQueryHeads heads, a share of the page's rows
   const int slice = (int(blockIdx.y) - kParts) / a.q_shares, share = int(blockIdx.y) - kParts - slice * a.q_shares;
   const int h0 = slice * kQueryHeads, heads = min(a.n_heads - h0, kQueryHeads);
-  if (blockIdx.x == 0 && share == 0 && tid < 64) {                       // rows before their sequence's first token: zeros
-    int reached = 0;
-    for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
-      int len;
-      const SeqRows m = lane_rows(c, a.r, s0, lane, reached, len);
-      for (int i = 0; i < m.count - len; ++i)
-        for (int j = 0; j < heads * c.rope; j += 8)
-          *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + (h0 + j / c.rope) * a.oH + j % c.rope) = make_uint4(0, 0, 0, 0);
-    }
-  }
   PageWork w = page_work(c, a.r, blockIdx.x);
-  if (w.seq < 0) return;
+  if (w.seq < 0) {                                                       // rows before their sequence's first token: zeros
+    early_rows(c, a.r, share, a.q_shares, [&](int64_t row) {
+      for (int j = 8 * tid; j < heads * c.rope; j += 8 * 256)
+        *reinterpret_cast<uint4*>(a.q_out + row * a.oT + (h0 + j / c.rope) * a.oH + j % c.rope) = make_uint4(0, 0, 0, 0);
+    });
+    return;
+  }
   const int rows = w.hi - w.lo, lo = w.lo;
   w.hi = lo + rows * (share + 1) / a.q_shares;
   w.lo = lo + rows * share / a.q_shares;
@@ -129,23 +125,14 @@ __global__ __launch_bounds__(256) void latent_read_kernel(LatentReadArgs a) {
     if (lane < lanes) reinterpret_cast<uint4*>(a.C + row * c.latent)[lane] = v;
     if (lane < more) reinterpret_cast<uint4*>(a.R + row * c.rope)[lane] = r;
   };
-  if (blockIdx.x == 0 && blockIdx.y == 0) {
-    check_rows(c, a.r);
-    if (wave == 0) {                                       // rows before their sequence's first token
-      int reached = 0;
-      for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
-        int len;
-        const SeqRows m = lane_rows(c, a.r, s0, lane, reached, len);
-        for (int l = 0; l < 64; ++l) {
-          const int first = __builtin_amdgcn_readlane(m.first, l);
-          const int early = __builtin_amdgcn_readlane(m.count - len, l), count = __builtin_amdgcn_readlane(m.count, l);
-          for (int i = 0; i < min(early, count); ++i) put(first + i, nullptr, 0);
-        }
-      }
-    }
-  }
+  if (blockIdx.x == 0 && blockIdx.y == 0) check_rows(c, a.r);
   const PageWork w = page_work(c, a.r, blockIdx.x);
-  if (w.seq < 0) return;
+  if (w.seq < 0) {                                         // rows before their sequence's first token
+    early_rows(c, a.r, int(blockIdx.y), kParts, [&](int64_t row) {
+      if (wave == 0) put(row, nullptr, 0);
+    });
+    return;
+  }
   const uint16_t* page = w.page < 0 ? nullptr : latent_at(c, w.page, a.layer);
   const int lo = max(w.lo, kPage / kParts * int(blockIdx.y)), hi = min(w.hi, kPage / kParts * int(blockIdx.y + 1));
   for (int slot = lo + wave; slot < hi; slot += 4) put(w.row0 + slot, page, slot);

@@ -197,13 +197,13 @@ __device__ inline int find_tile(const PagedView& c, const PagedRows& r, int flat
     const uint64_t above = __ballot(before + incl > flat);
     if (above) {
       const int l = __ffsll((unsigned long long)above) - 1;
-      const int start = before + __shfl(incl - n, l);
+      const int start = before + __builtin_amdgcn_readlane(incl - n, l);
       tile = flat - start;
       rows = {__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.count, l)};
       len = __builtin_amdgcn_readlane(own, l);
       return __builtin_amdgcn_readfirstlane(s0 + l);
     }
-    before += __shfl(incl, 63);
+    before += __builtin_amdgcn_readlane(incl, 63);
   }
   tile = 0;
   return -1;
@@ -245,10 +245,44 @@ __device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int
   return k;
 }
 
-// Workgroups in x for a call of n_rows rows: every touched page holds a row.
+// Workgroups in x for a call of n_rows rows: every touched page holds a row.  Where a
+// row precedes its sequence's first token, one of them at least has no page: that
+// sequence's pages begin with its rows, so that m rows touch (m + 63)/64 pages at most
+// and another's (m + 62)/64 + 1, and a row before the first token touches none.
 inline int64_t touched_bound(const PagedRows& r) {
   const int64_t by_pages = r.n_rows / kPage + 2 * int64_t(r.n_seqs);
   return r.n_rows < by_pages ? r.n_rows : by_pages;
+}
+
+// f(row) for the rows that precede their sequence's first token, by whole workgroups:
+// those without a page share them (a prompt whose reserve has failed has such rows
+// only; by a lane for each sequence 4096 rows of 16 heads took 33 ms).  share of
+// `shares`: of this workgroup among those of the same page.
+template <class F>
+__device__ inline void early_rows(const PagedView& c, const PagedRows& r, int share, int shares, F f) {
+  const int lane = threadIdx.x & 63;
+  int pages = 0, len;                                  // workgroups that have one
+  for (int s0 = 0, reached = 0; s0 < r.n_seqs; s0 += 64) {
+    const SeqRows m = lane_rows(c, r, s0, lane, reached, len);
+    pages += pages_touched(len, m.count);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) pages += __shfl_xor(pages, d);
+  const int step = (int(gridDim.x) - pages) * shares;
+  int at = (int(blockIdx.x) - pages) * shares + share; // of the early rows that are left
+  for (int s0 = 0, reached = 0; s0 < r.n_seqs; s0 += 64) {
+    const SeqRows m = lane_rows(c, r, s0, lane, reached, len);
+    const int early = m.count - min(len, m.count);
+    uint64_t who = __ballot(early > 0);
+    while (who) {
+      const int l = __ffsll((unsigned long long)who) - 1;
+      who &= who - 1;
+      const int first = __builtin_amdgcn_readlane(m.first, l), n = __builtin_amdgcn_readlane(early, l);
+#pragma unroll 1
+      for (; at < n; at += step) f(int64_t(first) + at);
+      at -= n;
+    }
+  }
 }
 
 // Starts that are no partition of rows, or rows before the first token.

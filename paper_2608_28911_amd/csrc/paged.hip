@@ -675,21 +675,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   write_page<D, G, BF, false>(a, RotaryArgs{}, w, codes, nullptr, blockIdx.z, a.parts, blockIdx.y);
 }
 
-// Rows before their sequence's first token have no position that the cache knows:
-// their queries are zeros.
-template <int D>
-__device__ inline void early_queries(const PagedAppendArgs& a) {
-  if (threadIdx.x >= 64) return;
-  int reached = 0;
-  for (int s0 = 0; s0 < a.w.r.n_seqs; s0 += 64) {
-    int len;
-    const SeqRows m = lane_rows(a.w.c, a.w.r, s0, threadIdx.x, reached, len);
-    for (int i = 0; i < m.count - len; ++i)
-      for (int j = 0; j < a.gqa * a.w.c.n_kv_heads * D; j += 8)
-        *reinterpret_cast<uint4*>(a.q_out + int64_t(m.first + i) * a.oT + j / D * a.oH + j % D) = make_uint4(0, 0, 0, 0);
-  }
-}
-
 // Write with the rotation on the way.  The workgroups of a page: for each kv head
 // its K, turned before it is quantized, and its V, as above; and as many or more for
 // the queries, each a share of the page's rows with every head, which lie together in
@@ -710,11 +695,20 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 5) void paged_append_kernel(Pag
     write_page<D, G, BF, true>(a.w, a.rot, w, codes, turns, blockIdx.z, a.w.parts, blockIdx.y);
     return;
   }
-  if (blockIdx.x == 0 && blockIdx.y == 0 && int(blockIdx.z) == a.w.parts) early_queries<D>(a);
   PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
-  if (w.seq < 0) return;
-  const int rows = w.hi - w.lo, lo = w.lo, shares = int(gridDim.y) * (int(gridDim.z) - a.w.parts);
+  const int shares = int(gridDim.y) * (int(gridDim.z) - a.w.parts);
   const int share = (int(blockIdx.z) - a.w.parts) * int(gridDim.y) + int(blockIdx.y);
+  if (w.seq < 0) {
+    // rows before their sequence's first token have no position that the cache knows:
+    // their queries are zeros
+    early_rows(a.w.c, a.w.r, share, shares, [&](int64_t row) {
+#pragma unroll 1
+      for (int j = 8 * threadIdx.x; j < a.gqa * a.w.c.n_kv_heads * D; j += 8 * 256)
+        *reinterpret_cast<uint4*>(a.q_out + row * a.oT + j / D * a.oH + j % D) = make_uint4(0, 0, 0, 0);
+    });
+    return;
+  }
+  const int rows = w.hi - w.lo, lo = w.lo;
   w.hi = lo + rows * (share + 1) / shares;
   w.lo = lo + rows * share / shares;
   if (w.lo >= w.hi) return;
@@ -752,26 +746,6 @@ __device__ inline void store8(void* p, int64_t at, const float (&v)[8]) {
   }
 }
 
-// Rows that would precede their sequence's first token: zeros.  Rare, so a
-// thread takes a whole sequence's, and one wave all of them.
-template <int D, int DT>
-__device__ inline void early_rows(const PagedReadArgs& a, int head) {
-  if (threadIdx.x >= 64) return;
-  const float zeros[8] = {};
-  int reached = 0;
-  for (int s0 = 0; s0 < a.r.n_seqs; s0 += 64) {
-    int len;
-    const SeqRows m = lane_rows(a.c, a.r, s0, threadIdx.x, reached, len);
-    for (int i = 0; i < m.count - len; ++i) {
-      const int64_t at = ((int64_t(blockIdx.z) * a.r.n_rows + m.first + i) * a.c.n_kv_heads + head) * D;
-      for (int j = 0; j < D; j += 8) {
-        store8<DT>(a.K, at + j, zeros);
-        store8<DT>(a.V, at + j, zeros);
-      }
-    }
-  }
-}
-
 // The record's words in LDS, with room between runs of 32 and of 256 words so
 // that the lanes of a row's neighbouring channels read from different banks.
 __device__ inline int spread(int word) { return word + (word >> 5) * 4 + (word >> 8) * 8; }
@@ -784,12 +758,16 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
   const PagedView& c = a.c;
   const int tid = threadIdx.x;
   const int layer = a.layer0 + blockIdx.z, head = blockIdx.y;
-  if (blockIdx.x == 0) {
-    if (blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
-    early_rows<D, DT>(a, head);
-  }
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(c, a.r);
   const PageWork w = page_work(c, a.r, blockIdx.x);
-  if (w.seq < 0) return;
+  if (w.seq < 0) {                                 // rows before their sequence's first token: zeros
+    early_rows(c, a.r, 0, 1, [&](int64_t row) {
+      const float zeros[8] = {};
+      if (tid < 2 * LPR)
+        store8<DT>(tid < LPR ? a.K : a.V, ((int64_t(blockIdx.z) * a.r.n_rows + row) * c.n_kv_heads + head) * D + tid % LPR * 8, zeros);
+    });
+    return;
+  }
   const uint4* src = reinterpret_cast<const uint4*>(paged_record_at(c, max(w.page, 0), layer, head));
   for (int i = tid; i < c.record / 16; i += 256)
     *reinterpret_cast<uint4*>(rec + spread(4 * i)) = w.page >= 0 ? src[i] : make_uint4(0, 0, 0, 0);

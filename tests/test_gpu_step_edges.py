@@ -86,3 +86,101 @@ def test_logits_that_rise_and_fall(dtype):
     t, b, v = S.choose(x.cpu().double().numpy(), np.float32([0.0, -1e-3]), 5)
     assert (got[1] == 2 * np.arange(200)[:, None] + b).all() and (got[2] == v).all()
     assert np.all(np.abs(got[0] - t) <= tolerance(t, vocab)), np.abs(got[0] - t).max()
+
+
+# ---- rows before their sequence's first token ----------------------------------
+
+def took(f, repeats=5):
+    """The smallest of some times of f, in us."""
+    import torch
+    f()
+    best = np.inf
+    for _ in range(repeats):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        b.synchronize()
+        best = min(best, 1e3 * a.elapsed_time(b))
+    return best
+
+
+def test_a_prompt_whose_reserve_has_failed():
+    """All of its rows precede the sequence's first token: their queries, and what is read, are zeros, written by the
+    whole grid (one lane for all of them took a thousand times as long as the prompt with room does)."""
+    import torch
+    from tests import pagedref as R
+    from tests.test_gpu_paged import ints, make, starts_of
+    n, h, hq = 4096, 2, 16
+    caches = make(h=h, hq=hq, n_pages=4, seqs=2, seq_pages=64), make(h=h, hq=hq, n_pages=64, seqs=2, seq_pages=64)
+    k, v = (torch.randn((n, h, 128), device="cuda").half() for _ in range(2))
+    q = torch.randn((n, hq, 128), device="cuda").half()
+    f, st = torch.from_numpy(S.frequencies(128)).cuda(), starts_of([0, n])
+    us = []
+    for c in caches:
+        c.reserve(ints([0, n]))
+        out = torch.full_like(q, 7.0)
+        us.append(took(lambda: c.append(0, k, v, st, f, q=q, q_out=out)))
+        back = tuple(torch.full((n, h, 128), 7.0, dtype=q.dtype, device="cuda") for _ in range(2))
+        us.append(took(lambda: c.read(0, st, n, out=back)))
+        if c is caches[0]:
+            assert c.status() == R.NO_PAGES | R.BAD_INDEX and c.lens.tolist() == [0, 0]
+            assert not out.any() and not back[0].any() and not back[1].any()
+        else:
+            assert c.status() == 0 and out.abs().amax(-1).all()
+    assert us[0] <= 20 * us[2] and us[1] <= 20 * us[3], us
+
+
+def test_a_prompt_of_latents_whose_reserve_has_failed():
+    import torch
+    from tests import pagedref as R
+    from tests.test_gpu_latent import make
+    from tests.test_gpu_paged import ints, starts_of
+    n, heads = 4096, 16
+    caches = [make(heads=heads, latent=256, rope=64, dtype="float16", n_pages=m, seqs=2, seq_pages=64, fill=0.0) for m in (4, 64)]
+    kv, q = torch.randn((n, 320), device="cuda").half(), torch.randn((n, heads, 64), device="cuda").half()
+    f, st = torch.from_numpy(S.frequencies(64)).cuda(), starts_of([n, 0])
+    us = []
+    for c in caches:
+        c.reserve(ints([n, 0]))
+        out = torch.full_like(q, 7.0)
+        us.append(took(lambda: c.append(0, kv[:, :256], kv[:, 256:], st, f, q=q, q_out=out)))
+        back = torch.full((n, 256), 7.0, dtype=q.dtype, device="cuda"), torch.full((n, 64), 7.0, dtype=q.dtype, device="cuda")
+        us.append(took(lambda: c.read(0, st, n, out=back)))
+        if c is caches[0]:
+            assert c.status() == R.NO_PAGES | R.BAD_INDEX
+            assert not out.any() and not back[0].any() and not back[1].any()
+        else:
+            assert c.status() == 0 and out.abs().amax(-1).all() and torch.equal(back[0], kv[:, :256])
+    assert us[0] <= 20 * us[2] and us[1] <= 20 * us[3], us
+
+
+@pytest.mark.parametrize("lens,counts", [
+    ([0], [1]), ([1], [2]), ([0, 5, 64], [1, 1, 1]), ([64, 3], [64, 70]), ([10, 0, 130, 1], [5, 100, 130, 1]),
+    ([63, 64, 65, 128], [64, 65, 66, 129]), ([0] * 70 + [9] * 70, [1] * 70 + [10, 1] * 35), ([200] * 3 + [0], [150, 1, 201, 300])])
+def test_rows_before_the_first_token_beside_others(lens, counts):
+    """Whoever has no page takes them: there is such a workgroup where there is such a row."""
+    import torch
+    from tests.test_gpu_latent import make as make_latents
+    from tests.test_gpu_paged import ints, make, starts_of
+    n, seqs = sum(counts), len(lens)
+    st, pages = starts_of(counts), 4 * seqs
+    early = np.concatenate([np.arange(m) < m - ln for ln, m in zip(lens, counts)])
+    early_d = torch.from_numpy(early).cuda()
+    a = make(h=3, hq=6, d=64, g=32, n_pages=pages, seqs=seqs, seq_pages=4)
+    b = make_latents(heads=5, latent=256, rope=32, dtype="float16", n_pages=pages, seqs=seqs, seq_pages=4, fill=1.0)
+    for c in (a, b):
+        c.reserve(ints(lens))
+    k, v, q = (torch.rand((n, m, 64), device="cuda").half() + 0.5 for m in (3, 3, 6))
+    out = torch.full((n + 3, 6, 64), 7.0, dtype=q.dtype, device="cuda")
+    a.append(0, k, v, st, torch.zeros(32, device="cuda"), q=q, q_out=out[:n])
+    assert torch.equal(out[:n], q.masked_fill(early_d[:, None, None], 0.0)) and (out[n:] == 7).all()
+    for x in a.read(0, st, n, out=tuple(torch.full((n, 3, 64), 7.0, device="cuda") for _ in range(2))):
+        assert not x[early_d].any() and (x[~early_d] > 0.4).all() and (x[~early_d] < 1.6).all()
+    kv, qr = torch.rand((n, 288), device="cuda").half() + 0.5, torch.rand((n, 5, 32), device="cuda").half() + 0.5
+    out = torch.full((n + 3, 5, 32), 7.0, dtype=q.dtype, device="cuda")
+    b.append(0, kv[:, :256], kv[:, 256:], st, torch.zeros(16, device="cuda"), q=qr, q_out=out[:n])
+    assert torch.equal(out[:n], qr.masked_fill(early_d[:, None, None], 0.0)) and (out[n:] == 7).all()
+    back = torch.full((n, 256), 7.0, dtype=q.dtype, device="cuda"), torch.full((n, 32), 7.0, dtype=q.dtype, device="cuda")
+    for x, want in zip(b.read(0, st, n, out=back), (kv[:, :256], kv[:, 256:])):
+        assert torch.equal(x, want.masked_fill(early_d[:, None], 0.0))
