@@ -44,12 +44,49 @@ def _float32():
     return _torch.float32
 
 
+def _extent(t):
+    """Bytes from a tensor's first element to the end of its last (0: it has none)."""
+    if t.numel() == 0:
+        return 0
+    return t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _runs(t):
+    """A tensor's elements as runs of so many bytes, and the steps between them: [(bytes, number)], the longest first."""
+    e = run = t.element_size()
+    steps = sorted((e * s, n) for n, s in zip(t.shape, t.stride()) if n > 1 and s > 0)
+    while steps and steps[0][0] <= run:
+        s, n = steps.pop(0)
+        run += s * (n - 1)
+    return run, steps[::-1]
+
+
 def _overlap(a, b):
-    """Whether the memory between two tensors' first and last elements meets."""
-    if a.numel() == 0 or b.numel() == 0:
+    """Whether an element of one tensor lies in the other: slices of one buffer that interleave do not meet.  (Said to
+    meet without a look at every step: ranges that do, of layouts unlike each other.)"""
+    ea, eb, apart = _extent(a), _extent(b), b.data_ptr() - a.data_ptr()
+    if not (ea and eb and -eb < apart < ea):
         return False
-    end = lambda t: t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))  # noqa: E731
-    return a.data_ptr() < end(b) and b.data_ptr() < end(a)
+    left = 1000                                                      # steps to look at
+
+    def meet(d, ra, sa, rb, sb):                                     # b's runs are d bytes behind a's
+        nonlocal left
+        if not sa and not sb:
+            return -rb < d < ra
+        s = max(sa[0][0] if sa else 0, sb[0][0] if sb else 0)        # the longest step: of one, or of both
+        na = nb = 1
+        if sa and sa[0][0] == s:
+            na, sa = sa[0][1], sa[1:]
+        if sb and sb[0][0] == s:
+            nb, sb = sb[0][1], sb[1:]
+        wa, wb = (r + sum(t * (n - 1) for t, n in rest) for r, rest in ((ra, sa), (rb, sb)))
+        for k in range(max(1 - na, -((wb + d - 1) // s)), min(nb - 1, (wa - d - 1) // s) + 1):
+            left -= 1
+            if left < 0 or meet(d + k * s, ra, sa, rb, sb):
+                return True
+        return False
+
+    return meet(apart, *_runs(a), *_runs(b))
 
 
 _torch = None
@@ -161,8 +198,8 @@ class _Paged:
         return _abi.Rotary(freqs.data_ptr(), None if positions is None else self._ints(positions, "positions", n),
                            2 * freqs.numel(), 1 if interleaved else 0)
 
-    def _turned(self, q, q_out, n, heads, dim, dtype):
-        """Where query rows are turned to, and the addresses and strides of both."""
+    def _turned(self, q, q_out, n, heads, dim, dtype, *others):
+        """Where query rows are turned to, and the addresses and strides of both; others: the call's other inputs."""
         if q is None:
             _need(q_out is None, "q_out: there is no q")
             return None, _NO_QUERIES
@@ -176,9 +213,11 @@ class _Paged:
         _need(q_out.shape == shape and so[2] == 1 and q_out.dtype == dtype and q_out.get_device() == self._at,
               "q_out: of q's shape and dtype with a unit channel stride")
         # rows and heads apart from each other, and all of it from q unless it is q
-        _need(so[1] >= dim and so[0] >= heads * so[1] or so[0] >= dim and so[1] >= n * so[0] or n == 1 and so[1] >= dim
-              or heads == 1 and so[0] >= dim or n * heads <= 1, "q_out: rows that overlap")
+        _need(so[1] >= dim and so[0] >= (heads - 1) * so[1] + dim or so[0] >= dim and so[1] >= (n - 1) * so[0] + dim
+              or n == 1 and so[1] >= dim or heads == 1 and so[0] >= dim or n * heads <= 1, "q_out: rows that overlap")
         _need(to == at and so == st or not _overlap(q, q_out), "q_out: q itself, or apart from q")
+        for t in others:
+            _need(t is None or not _overlap(t, q_out), "q_out: apart from the call's other inputs")
         return q_out, (at, st[0], st[1], to, so[0], so[1])
 
     # -- pages -------------------------------------------------------------
@@ -252,7 +291,7 @@ class PagedKV4(_Paged):
         quantized; V as it is.  Pair i of a row's first 2 len(freqs) channels (channels i and i + len(freqs), or 2i and
         2i+1: interleaved) turns by position * freqs[i] (fp32); positions: int32 [n], or None: the row's place in its
         sequence.  q [n, n_q_heads, head_dim] (a unit channel stride) is turned likewise and returned, in q_out if
-        given, which may be q itself (None without q)."""
+        given, which may be q itself, and holds no element of another input (None without q)."""
         code = _code(K.dtype, "K")
         shape, st = K.shape, K.stride()
         _need(V.dtype == K.dtype and V.shape == shape and V.stride() == st
@@ -261,7 +300,7 @@ class PagedKV4(_Paged):
               "K, V: [n, %d, %d] alike, with a unit channel stride, on %s", self._heads, self._dim, self.device)
         n = shape[0]
         rot = self._rotary(freqs, positions, interleaved, n)
-        out, turned = self._turned(q, q_out, n, self._q_heads, self._dim, K.dtype)
+        out, turned = self._turned(q, q_out, n, self._q_heads, self._dim, K.dtype, K, V, starts, freqs, positions)
         at, n_seqs = self._starts(starts)
         _enqueue(self._at, self._lib.semkv_paged_append, "semkv_paged_append", self._ref, layer, K.data_ptr(), V.data_ptr(),
                  code, st[0], st[1], *turned, ctypes.byref(rot), at, n_seqs, n)
@@ -360,7 +399,7 @@ class PagedLatent(_Paged):
         n = C.shape[0]
         c, r = self._part(C, "C", (n, self._latent)), self._part(R, "R", (n, self._rope))
         rot = self._rotary(freqs, positions, interleaved, n)
-        out, turned = self._turned(q, q_out, n, self._heads, self._rope, self.dtype)
+        out, turned = self._turned(q, q_out, n, self._heads, self._rope, self.dtype, C, R, starts, freqs, positions)
         at, n_seqs = self._starts(starts)
         _enqueue(self._at, self._lib.semkv_latent_append, "semkv_latent_append", self._ref, layer, C.data_ptr(), c[0],
                  R.data_ptr(), r[0], *turned, ctypes.byref(rot), at, n_seqs, n)
