@@ -552,7 +552,8 @@ int semkv_latent_read(const semkv_latent* c, int32_t layer, void* C, void* R, co
  * 8.  out: the same dtype, contiguous [n_rows][n_heads][latent], 16-byte aligned,
  * apart from q_rope, and from q or q itself where that is contiguous; lse: fp32
  * [n_rows][n_heads] or NULL.  scale: positive and finite.
- * (A score that fp32 does not hold makes its row NaN.)
+ * (Scores that fp32 does not hold: one of +inf or NaN makes its row NaN; one of -inf
+ * has weight 0, and a row that has no others gives what one that sees no token does.)
  * The weights p_t enter the second product rounded to the cache's type: out is off by
  * at most 2^-8 (bf16) or 2^-11 (fp16) sum_t p_t |c_t|, in fp16 by 2^-35 of the
  * largest weight times |c_t| for each token of less than 2^-24 of it, by what fp32

@@ -184,3 +184,43 @@ def test_rows_before_the_first_token_beside_others(lens, counts):
     back = torch.full((n, 256), 7.0, dtype=q.dtype, device="cuda"), torch.full((n, 32), 7.0, dtype=q.dtype, device="cuda")
     for x, want in zip(b.read(0, st, n, out=back), (kv[:, :256], kv[:, 256:])):
         assert torch.equal(x, want.masked_fill(early_d[:, None], 0.0))
+
+
+# ---- attention over latents -------------------------------------------------------
+
+@pytest.mark.parametrize("heads", [4, 20, 64])
+def test_infinite_scores(heads):
+    """A score of +inf or NaN makes its row NaN, one of -inf has no weight; only such: as a row that sees nothing."""
+    import torch
+    from tests.test_gpu_latent import make, rows
+    from tests.test_gpu_paged import ints, starts_of
+    rng = np.random.default_rng(heads)
+    n, inf = 700, float("inf")
+    cache = make(heads=heads, latent=256, rope=32, dtype="bfloat16", n_pages=16, seqs=2, seq_pages=12)
+    cache.reserve(ints([n, 0]))
+    kv = rows(rng, (n, 288), "bfloat16")
+    kv[:, 0], kv[:, 1] = 1.0, 0.0
+    kv[::3, 1], kv[5, 1] = 4.0, 4.0
+    cache.append(0, kv[:, :256], kv[:, 256:], starts_of([n, 0]), torch.zeros(16, device="cuda"))
+    q, qr = rows(rng, (3, heads, 256), "bfloat16"), rows(rng, (3, heads, 32), "bfloat16")
+    q[..., :2] = 0.0
+    q[0, ::2, 0], q[1, ::2, 0], q[1, 1::2, 0], q[2, :, 1] = -inf, inf, float("nan"), -3e38      # -1.2e39 of every third token
+    out, lse = cache.attn(0, q, qr, starts_of([3, 0]), 0.06, with_lse=True)
+    assert cache.status() == 0
+    assert not out[0, ::2].any() and (lse[0, ::2] == -inf).all()
+    assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
+    c, r = (t.cpu().double().numpy() for t in (kv[:, :256], kv[:, 256:]))
+    for i, some in ((0, range(1, heads, 2)), (2, range(heads))):
+        seen = np.arange(n - 2 + i)
+        if i == 2:
+            seen = seen[(seen % 3 != 0) & (seen != 5)]
+        for h in some:
+            a, b = q[i, h].cpu().double().numpy(), qr[i, h].cpu().double().numpy()
+            a[1] = 0.0
+            want, wl, p = S.attend(a, b, c[seen], r[seen], 0.06)
+            # scores' roundings (288 products, two operations, and the exponent's), the weights', the sums', the output's
+            x = 0.06 * (np.abs(c[seen]) @ np.abs(a) + np.abs(r[seen]) @ np.abs(b)).max()
+            d = (296 + 3) * U * x + 48 * U
+            tol = (2.0 ** -8 + 2 * d + n * U) * (p @ np.abs(c[seen])) + (2.0 ** -8 + d + n * U) * np.abs(want)
+            assert np.all(np.abs(out[i, h].cpu().double().numpy() - want) <= tol)
+            assert abs(lse[i, h].item() - wl) <= 2 * d + n * U + U * abs(wl)
