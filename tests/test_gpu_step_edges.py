@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from tests import stepref as S
+from tests.test_gpu_paged import ints, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -110,7 +111,7 @@ def test_a_prompt_whose_reserve_has_failed():
     whole grid (one lane for all of them took a thousand times as long as the prompt with room does)."""
     import torch
     from tests import pagedref as R
-    from tests.test_gpu_paged import ints, make, starts_of
+    from tests.test_gpu_paged import make
     n, h, hq = 4096, 2, 16
     caches = make(h=h, hq=hq, n_pages=4, seqs=2, seq_pages=64), make(h=h, hq=hq, n_pages=64, seqs=2, seq_pages=64)
     k, v = (torch.randn((n, h, 128), device="cuda").half() for _ in range(2))
@@ -135,7 +136,6 @@ def test_a_prompt_of_latents_whose_reserve_has_failed():
     import torch
     from tests import pagedref as R
     from tests.test_gpu_latent import make
-    from tests.test_gpu_paged import ints, starts_of
     n, heads = 4096, 16
     caches = [make(heads=heads, latent=256, rope=64, dtype="float16", n_pages=m, seqs=2, seq_pages=64, fill=0.0) for m in (4, 64)]
     kv, q = torch.randn((n, 320), device="cuda").half(), torch.randn((n, heads, 64), device="cuda").half()
@@ -162,7 +162,7 @@ def test_rows_before_the_first_token_beside_others(lens, counts):
     """Whoever has no page takes them: there is such a workgroup where there is such a row."""
     import torch
     from tests.test_gpu_latent import make as make_latents
-    from tests.test_gpu_paged import ints, make, starts_of
+    from tests.test_gpu_paged import make
     n, seqs = sum(counts), len(lens)
     st, pages = starts_of(counts), 4 * seqs
     early = np.concatenate([np.arange(m) < m - ln for ln, m in zip(lens, counts)])
@@ -193,7 +193,6 @@ def test_infinite_scores(heads):
     """A score of +inf or NaN makes its row NaN, one of -inf has no weight; only such: as a row that sees nothing."""
     import torch
     from tests.test_gpu_latent import make, rows
-    from tests.test_gpu_paged import ints, starts_of
     rng = np.random.default_rng(heads)
     n, inf = 700, float("inf")
     cache = make(heads=heads, latent=256, rope=32, dtype="bfloat16", n_pages=16, seqs=2, seq_pages=12)
@@ -224,3 +223,69 @@ def test_infinite_scores(heads):
             tol = (2.0 ** -8 + 2 * d + n * U) * (p @ np.abs(c[seen])) + (2.0 ** -8 + d + n * U) * np.abs(want)
             assert np.all(np.abs(out[i, h].cpu().double().numpy() - want) <= tol)
             assert abs(lse[i, h].item() - wl) <= 2 * d + n * U + U * abs(wl)
+
+
+@pytest.mark.parametrize("dtype,heads,latent,rope", [("bfloat16", 16, 512, 64), ("float16", 7, 256, 32), ("float16", 16, 512, 32)])
+def test_slots_without_rows_beside_a_chunk(dtype, heads, latent, rope):
+    """The height of attention's tiles goes by the rows a slot has on average: the same chunk among 1 to 64 slots takes
+    tiles of 64, 32 and 16 rows, and each of them is held to 64 bits."""
+    from tests.test_gpu_latent import check, fill, make, rows
+    rng = np.random.default_rng(heads + latent)
+    cache = make(heads=heads, latent=latent, rope=rope, dtype=dtype, n_pages=16, seqs=64, seq_pages=16)
+    m, n = 60, 900
+    fill(cache, rng, [n])
+    q, qr = rows(rng, (m, heads, latent), dtype), rows(rng, (m, heads, rope), dtype)
+    heights = set()
+    for slots in (1, 40, 64):
+        counts = [m] + [0] * (slots - 1)
+        per = -(-m * heads // slots)
+        heights.add(16 if per <= 16 else 32 if per <= 32 else 64)
+        out, lse = cache.attn(0, q, qr, starts_of(counts), 0.05, with_lse=True)
+        check(cache, q, qr, [m], 0.05, out, lse)
+    assert len(heights) == (3 if heads == 16 else 2)
+    assert cache.status() == 0
+
+
+@pytest.mark.parametrize("heads,lens", [
+    (16, [40000]),                                           # as many splits as a tile may have
+    (40, [33000]),
+    (16, [int(x) for x in np.random.default_rng(1).integers(100, 3000, 40)]),     # shares that have to grow until they suffice
+    (64, [int(x) for x in np.random.default_rng(2).integers(1, 2000, 60)]),
+    (20, [int(x) for x in np.random.default_rng(3).integers(1, 1500, 100)])])     # more sequences than a wave has lanes
+def test_splits_of_many_lengths(heads, lens):
+    from tests.test_gpu_latent import attend, check, fill, make
+    rng = np.random.default_rng(heads)
+    pages = sum((n + 63) // 64 for n in lens)
+    cache = make(heads=heads, latent=256, rope=32, dtype="float16", n_pages=pages, seqs=len(lens), seq_pages=(max(lens) + 63) // 64)
+    fill(cache, rng, lens)
+    counts = [1] * len(lens)
+    q, qr, scale, out, lse = attend(cache, rng, counts)
+    some = None if len(lens) == 1 else set(range(0, len(lens), 7)) | {int(np.argmin(lens)), int(np.argmax(lens))}
+    check(cache, q, qr, counts, scale, out, lse, some=some)
+    again = cache.attn(0, q, qr, starts_of(counts), scale, with_lse=True)
+    assert (again[0] == out).all() and (again[1] == lse).all() and cache.status() == 0
+
+
+def test_compact_of_latents_whose_page_is_missing():
+    """Tokens kept from a missing page are zeros, and reported; the others move."""
+    import torch
+    from tests import pagedref as R
+    from tests.test_gpu_latent import make, rows
+    rng = np.random.default_rng(3)
+    cache = make(heads=1, latent=512, rope=32, dtype="float16", n_layers=2, n_pages=12, seqs=2, seq_pages=4)
+    cache.reserve(ints([200, 30]))
+    f, kv = torch.zeros(16, device="cuda"), [rows(rng, (230, 544), "float16") for _ in range(2)]
+    for layer in range(2):
+        cache.append(layer, kv[layer][:, :512], kv[layer][:, 512:], starts_of([200, 30]), f)
+    table = cache.table.clone()
+    table[0, 1] = -1                                          # tokens 64 .. 127
+    cache.assign(cache.lens.clone(), table)
+    cache.status_word.zero_()
+    kept = sorted(rng.permutation(200)[:90].tolist())
+    cache.compact(ints([kept, [0] * 90]), ints([90, -1]))
+    assert cache.status() == R.BAD_INDEX and cache.lens.tolist() == [90, 30] and cache.refs.sum().item() == 3
+    gone = torch.tensor([64 <= t < 128 for t in kept], device="cuda")
+    for layer in range(2):
+        c, r = cache.read(layer, starts_of([90, 30]), 120)
+        want = torch.cat((kv[layer][kept].masked_fill(gone[:, None], 0.0), kv[layer][200:]))
+        assert torch.equal(c, want[:, :512]) and torch.equal(r, want[:, 512:])
