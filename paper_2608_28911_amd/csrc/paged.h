@@ -197,13 +197,13 @@ __device__ inline int find_tile(const PagedView& c, const PagedRows& r, int flat
     const uint64_t above = __ballot(before + incl > flat);
     if (above) {
       const int l = __ffsll((unsigned long long)above) - 1;
-      const int start = before + __builtin_amdgcn_readlane(incl - n, l);
+      const int start = before + __shfl(incl - n, l);
       tile = flat - start;
       rows = {__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.count, l)};
       len = __builtin_amdgcn_readlane(own, l);
       return __builtin_amdgcn_readfirstlane(s0 + l);
     }
-    before += __builtin_amdgcn_readlane(incl, 63);
+    before += __shfl(incl, 63);
   }
   tile = 0;
   return -1;
@@ -245,6 +245,16 @@ __device__ inline PageWork page_work(const PagedView& c, const PagedRows& r, int
   return k;
 }
 
+// The same, in scalar registers.
+__device__ inline PageWork uniform(PageWork k) {
+  k.lo = __builtin_amdgcn_readfirstlane(k.lo);
+  k.hi = __builtin_amdgcn_readfirstlane(k.hi);
+  k.first = __builtin_amdgcn_readfirstlane(k.first);
+  k.row0 = int64_t(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(k.row0 >> 32)))) << 32 |
+                   uint32_t(__builtin_amdgcn_readfirstlane(int(k.row0))));
+  return k;
+}
+
 // Workgroups in x for a call of n_rows rows: every touched page holds a row.  Where a
 // row precedes its sequence's first token, one of them at least has no page: that
 // sequence's pages begin with its rows, so that m rows touch (m + 63)/64 pages at most
@@ -262,10 +272,13 @@ template <class F>
 __device__ inline void early_rows(const PagedView& c, const PagedRows& r, int share, int shares, F f) {
   const int lane = threadIdx.x & 63;
   int pages = 0, len;                                  // workgroups that have one
+  bool some = false;
   for (int s0 = 0, reached = 0; s0 < r.n_seqs; s0 += 64) {
     const SeqRows m = lane_rows(c, r, s0, lane, reached, len);
     pages += pages_touched(len, m.count);
+    some = some || m.count > len;
   }
+  if (!__any(some)) return;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) pages += __shfl_xor(pages, d);
   const int step = (int(gridDim.x) - pages) * shares;

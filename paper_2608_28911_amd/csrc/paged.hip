@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 5) void paged_append_kernel(Pag
     write_page<D, G, BF, true>(a.w, a.rot, w, codes, turns, blockIdx.z, a.w.parts, blockIdx.y);
     return;
   }
-  PageWork w = page_work(a.w.c, a.w.r, blockIdx.x);
+  PageWork w = uniform(page_work(a.w.c, a.w.r, blockIdx.x));
   const int shares = int(gridDim.y) * (int(gridDim.z) - a.w.parts);
   const int share = (int(blockIdx.z) - a.w.parts) * int(gridDim.y) + int(blockIdx.y);
   if (w.seq < 0) {
