@@ -90,8 +90,8 @@ __device__ inline uint4 load_anywhere(const char* p) {
 // workgroup, bounds what it can keep, and the few lanes that reach it (k, and what
 // ties) are looked through again, a lane's vectors across the wave; what reaches the
 // bound is put in order by counting.  (A list kept on the way took 33 us for 256 rows
-// of 128000 fp16 logits and k = 8, half of its vector instructions insertions; now 18.9,
-// of which 12 go with the logits, 5.4 TB/s.)
+// of 128000 fp16 logits and k = 8, half of its vector instructions insertions; now 18.9 to
+// 19.3, of which 12 go with the logits, 5.4 TB/s.)
 template <int DT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void beam_rows_kernel(BeamArgs a) {
   constexpr int V = Elem<DT>::vec, NT = 64 * WAVES, U = 4;

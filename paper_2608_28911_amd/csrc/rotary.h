@@ -18,7 +18,8 @@ struct RotaryArgs {
   int32_t dim, interleaved;      // channels turned; pairs (2i, 2i+1), else (i, i + dim/2)
 };
 
-// cos and sin of p f, rounded to 32 bits.  k, the nearest whole number of quarter
+// cos and sin of p f, rounded to 32 bits: Cody and Waite's reduction, then Taylor's
+// series.  k, the nearest whole number of quarter
 // turns, comes out of an addition that leaves no bits below the point (its lowest
 // bits say which quarter); the angle is reduced to [-pi/4, pi/4] by two parts of
 // pi/2 (exact products in fused multiply-adds: k has at most 31 bits), then both
